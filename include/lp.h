@@ -28,7 +28,7 @@
  *     are ADDED to: the caller clears them when a fresh count is wanted.
  *   - Every argument is validated before anything is launched; a call that
  *     returns anything but LP_OK has launched nothing.  Errors are return codes
- *     only.  Device pointers must be aligned to 16 bytes.
+ *     only.  Device pointers must be aligned to 16 bytes (the microscaled calls say where less will do).
  */
 #ifndef LP_H
 #define LP_H
@@ -313,6 +313,112 @@ lp_status lp_fc_fwd(int M, int K, int Nout, const void *x_codes_dev, lp_qfmt qx,
  */
 lp_status lp_maxpool2x2(const void *x_codes_dev, void *y_codes_dev, int N, int H, int W, int C,
                         int n_bits, void *stream);
+
+/*
+ * Microscaled formats: linear layers in 4-bit floating point, and activations kept in 8 bits for the
+ * backward pass.  Where a Qm.f tensor has one point for all its values (Sec. 2.3), these have one for
+ * every 32 neighbours of a row, held in a byte e that stands for 2^(e - 127).
+ *
+ *   mx4    elements of sign, two exponent bits and one mantissa bit: code 0..7 = 0, .5, 1, 1.5, 2, 3, 4,
+ *          6, bit 3 the sign; value = element * 2^(e - 127).  codes [rows][16 * B] bytes, two elements a
+ *          byte, element 2i in the low half of byte i; scales [rows][B] bytes; B = 8 * ceil(cols / 256)
+ *          blocks of 32, so that rows are whole groups of 256 elements.  Readers ask for scale bytes of
+ *          2..252 and for padding elements of code 0 (any scale byte in range); lp_mx4_quantize writes both.
+ *   ckpt8  elements are integers -127..127; value = element * 2^(e - 133).  codes [rows][32 * B] int8,
+ *          scales [rows][B] bytes, B = ceil(cols / 32).  Scale bytes of 7..254; padding elements 0.
+ *
+ * The quantizers place a block's point from its largest finite magnitude, of biased exponent E (that of the
+ * value in 32 bits): mx4 e = E - 2, kept within 2..252 (the usual rule of this format: the largest value
+ * lies in [4, 8) and saturates above 6); ckpt8 e = E, kept within 7..254 (the largest lies in [64, 128)).
+ * Every value of either format is a normal number of 32 bits or zero, so smaller magnitudes round to zero.
+ * As in lp_quantize NaN becomes 0 and what does not fit saturates, infinities included.  The sign of
+ * zero is kept by mx4.
+ *
+ * Float tensors (x, y, dy, dx, dw) are row-major with their own row stride ld >= columns, in elements; they
+ * and the bias need the alignment of their type only.  Codes are aligned to 16 bytes, mx4 scales to 8, ckpt8
+ * scales not at all.  Columns beyond a row's last are neither read nor written.  No tensor may
+ * overlap another one of the call unless its text says so.  Calls without rows do
+ * nothing and return LP_OK.
+ */
+typedef enum { LP_F32 = 0, LP_BF16 = 1, LP_F16 = 2 } lp_dtype;
+
+/* Activation functions: max(h, 0); h * s(h), s the logistic function; h * s(2 u),
+ * u = sqrt(2 / pi) * (h + 0.044715 h^3).  NaN stays NaN, at -Inf the last two are 0. */
+typedef enum { LP_ACT_NONE = 0, LP_ACT_RELU = 1, LP_ACT_SILU = 2, LP_ACT_GELU_TANH = 3 } lp_actfn;
+
+/* Bytes of an mx4 / ckpt8 tensor's two parts. */
+lp_status lp_mx4_bytes(size_t rows, size_t cols, size_t *codes_bytes_host, size_t *scales_bytes_host);
+lp_status lp_ckpt8_bytes(size_t rows, size_t cols, size_t *codes_bytes_host, size_t *scales_bytes_host);
+
+/*
+ * lp_mx4_quantize -- rows x cols floats to mx4.  r as in lp_quantize, on the grid of the eight magnitudes
+ * (halfway cases away from zero, to the even code, or up with the probability of the remainder: the
+ * magnitude's distance from the magnitude below, over the distance of the two, is compared with the draw of
+ * element row * cols + col as lp_quantize draws it).  zero_count_dev / sat_count_dev (nullable): += values
+ * with a zero magnitude / values clipped at 6.  LP_EUNSUPPORTED: 2^34 padded elements
+ * or more, or 2^31 rows or columns.
+ * lp_mx4_dequantize -- the values, rounded to yt (nearest even; f16 may overflow to infinity).
+ */
+lp_status lp_mx4_quantize(const void *x_dev, lp_dtype xt, size_t rows, size_t cols, size_t ldx, void *codes_dev,
+                          void *scales_dev, lp_round r, uint64_t seed, uint64_t *zero_count_dev,
+                          uint64_t *sat_count_dev, void *stream);
+lp_status lp_mx4_dequantize(const void *codes_dev, const void *scales_dev, size_t rows, size_t cols, void *y_dev,
+                            lp_dtype yt, size_t ldy, void *stream);
+
+/*
+ * lp_mx4_fc_fwd -- y = act(Xq Wq^T + bias), the inner product of mx4 values on the scaled matrix instructions:
+ *   x_dev         [M][K] floats of type xt with row stride ldx, brought to mx4 by the call (nearest even), or,
+ *                 where x_scales_dev is given, the codes of an mx4 tensor (xt and ldx are not looked at)
+ *   w_codes_dev, w_scales_dev   mx4 [Nout][K], as lp_mx4_quantize leaves it: nothing is packed
+ *   bias_dev      nullable, Nout floats of 32 bits
+ *   y_dev         [M][Nout] of type yt, row stride ldy
+ * Products and sums are held in 32 bits and rounded once.  The order of the sums depends on
+ * M, K and Nout alone: equal calls give equal bits.  The workspace (lp_mx4_fc_workspace_bytes, may be 0; then it may be
+ * null) needs no initialisation and carries nothing from call to call; calls that share one must not
+ * overlap in time.  LP_EUNSUPPORTED: M, K or Nout above 2^24.
+ */
+lp_status lp_mx4_fc_workspace_bytes(int M, int K, int Nout, size_t *bytes_host);
+lp_status lp_mx4_fc_fwd(int M, int K, int Nout, const void *x_dev, lp_dtype xt, size_t ldx, const void *x_scales_dev,
+                        const void *w_codes_dev, const void *w_scales_dev, const float *bias_dev, void *y_dev,
+                        lp_dtype yt, size_t ldy, lp_actfn act, void *workspace_dev, size_t workspace_bytes,
+                        void *stream);
+
+/*
+ * lp_mx4_fc_dgrad -- gradient of that product with respect to its input, the rounding of X passed through:
+ * dX = dY Wq, dY [M][Nout] in bfloat16 (row stride lddy), dX [M][K] of type dxt (bfloat16 or 32 bits; LP_F16:
+ * LP_EUNSUPPORTED).  The mx4 values are exact in bfloat16; sums in 32 bits.  Workspace, order and limits as above.
+ */
+lp_status lp_mx4_fc_dgrad_workspace_bytes(int M, int K, int Nout, size_t *bytes_host);
+lp_status lp_mx4_fc_dgrad(int M, int K, int Nout, const void *dy_dev, size_t lddy, const void *w_codes_dev,
+                          const void *w_scales_dev, void *dx_dev, lp_dtype dxt, size_t lddx, void *workspace_dev,
+                          size_t workspace_bytes, void *stream);
+
+/*
+ * lp_ckpt8_save -- keeps rows x cols floats as ckpt8 for the backward pass and, where y_dev is given, writes
+ * y = act(x) (same type as x, row stride ldy; y_dev may be x_dev if ldy == ldx) in the same pass.  r as in lp_quantize.
+ * lp_ckpt8_load -- the kept values, rounded to yt (nearest even).
+ * lp_ckpt8_act_bwd -- dx = dy * act'(kept value); dy and dx of type t, dx_dev may be dy_dev if the strides are equal.
+ * At 0 the slope of LP_ACT_RELU is 0.  LP_EUNSUPPORTED as lp_mx4_quantize.
+ */
+lp_status lp_ckpt8_save(const void *x_dev, lp_dtype xt, size_t rows, size_t cols, size_t ldx, void *codes_dev,
+                        void *scales_dev, lp_round r, uint64_t seed, lp_actfn act, void *y_dev, size_t ldy,
+                        void *stream);
+lp_status lp_ckpt8_load(const void *codes_dev, const void *scales_dev, size_t rows, size_t cols, void *y_dev,
+                        lp_dtype yt, size_t ldy, void *stream);
+lp_status lp_ckpt8_act_bwd(const void *codes_dev, const void *scales_dev, size_t rows, size_t cols, const void *dy_dev,
+                           lp_dtype t, size_t lddy, lp_actfn act, void *dx_dev, size_t lddx, void *stream);
+
+/*
+ * lp_ckpt8_fc_wgrad -- gradient of an inner product with respect to its weights and bias from the kept input:
+ * dW[o][k] = sum_b dY[b][o] X8[b][k] (+ dW if accumulate), dbias[o] = sum_b dY[b][o] (+ dbias).  dY [M][Nout] in
+ * bfloat16, X8 ckpt8 [M][K], dW [Nout][K] of type dwt (bfloat16 or 32 bits; LP_F16: LP_EUNSUPPORTED), dbias_dev
+ * nullable, Nout floats of 32 bits.  The ckpt8 values are exact in bfloat16; sums in 32 bits.  M == 0 is allowed:
+ * the sums are zero.  Workspace, order and limits as lp_mx4_fc_fwd.
+ */
+lp_status lp_ckpt8_fc_wgrad_workspace_bytes(int M, int K, int Nout, size_t *bytes_host);
+lp_status lp_ckpt8_fc_wgrad(int M, int K, int Nout, const void *dy_dev, size_t lddy, const void *x_codes_dev,
+                            const void *x_scales_dev, void *dw_dev, lp_dtype dwt, size_t lddw, float *dbias_dev,
+                            int accumulate, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -6,7 +6,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblp.so")
-SOURCES = ["lp_elementwise.hip", "lp_conv.hip", "lp_fc.hip"]
+SOURCES = ["lp_elementwise.hip", "lp_conv.hip", "lp_fc.hip", "lp_mx.hip", "lp_mx_fc.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -20,28 +20,6 @@ static int grid_for(size_t groups)
     return (int)blocks;
 }
 
-// Adds a block's counts to the caller's counters (either may be null): the waves' totals meet in LDS
-// and the block issues one atomic per counter.  The atomics of a launch all hit one address and are
-// served one after the other, 12 to 14 ns each: with one per wave and counter (16 k of them) a counting
-// lp_quantize of 25.7 M elements took 207 us instead of 29, a counting lp_act to 8 bits (32 k) 398 instead of 44.
-template <int THREADS>
-__device__ __forceinline__ void add_block_counts(unsigned zeros, unsigned sats, unsigned long long *zero_count,
-                                                 unsigned long long *sat_count)
-{
-    __shared__ unsigned part[2][THREADS / 64];
-    if ((threadIdx.x & 63) == 0) {
-        part[0][threadIdx.x >> 6] = zeros;
-        part[1][threadIdx.x >> 6] = sats;
-    }
-    __syncthreads();
-    if (threadIdx.x < 2) {
-        unsigned total = 0;
-        for (int w = 0; w < THREADS / 64; ++w) total += part[threadIdx.x][w];
-        unsigned long long *out = threadIdx.x ? sat_count : zero_count;
-        if (out && total) atomicAdd(out, (unsigned long long)total);
-    }
-}
-
 // Counting launches: one block of sixteen waves per CU, so that at most 256 atomics per counter
 // are left and hide behind the streaming.  Measured on 25.7 M / 5.1 M elements, lp_quantize with
 // counters: 256 x 1024 threads 29 / 11 us, 512 x 512 30 / 12, 512 x 256 36 / 12.5, 1024 x 256 37 / 17,
@@ -78,39 +56,6 @@ __device__ __forceinline__ V load16(const V *p)
 {
     if constexpr (ONCE) return __builtin_nontemporal_load(p);
     else return *p;
-}
-
-// ------------------------------------------------------------------ Philox4x32-10
-// Counter-based generator of Salmon, Moraes, Dror, Shaw (SC'11): ten rounds of two
-// 32x32->64 multiplies and xors, key bumped by the Weyl constants each round.  One block gives four
-// words; element i of a tensor draws word i % 4 of the block with counter (i / 4, 0).
-struct PhiloxBlock {
-    uint32_t w[4];
-};
-__device__ __forceinline__ PhiloxBlock philox4x32_10(uint64_t ctr, uint64_t key)
-{
-    uint32_t c0 = (uint32_t)ctr, c1 = (uint32_t)(ctr >> 32), c2 = 0, c3 = 0;
-    uint32_t k0 = (uint32_t)key, k1 = (uint32_t)(key >> 32);
-#pragma unroll
-    for (int i = 0; i < 10; ++i) {
-        const uint64_t p0 = (uint64_t)0xD2511F53u * c0;
-        const uint64_t p1 = (uint64_t)0xCD9E8D57u * c2;
-        const uint32_t n0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
-        const uint32_t n1 = (uint32_t)p1;
-        const uint32_t n2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
-        const uint32_t n3 = (uint32_t)p0;
-        c0 = n0; c1 = n1; c2 = n2; c3 = n3;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
-    }
-    return PhiloxBlock{{c0, c1, c2, c3}};
-}
-// the draw of element i by itself (ragged tails)
-__device__ __forceinline__ uint32_t philox_draw(uint64_t i, uint64_t key)
-{
-    const PhiloxBlock b = philox4x32_10(i >> 2, key);
-    const unsigned k = (unsigned)i & 3u;
-    return k == 0 ? b.w[0] : k == 1 ? b.w[1] : k == 2 ? b.w[2] : b.w[3];
 }
 
 // ------------------------------------------------------------------------ quantize

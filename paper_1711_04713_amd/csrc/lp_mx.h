@@ -1,0 +1,133 @@
+// Pieces shared by the kernels of the microscaled formats (mx4: 4-bit floating point, ckpt8: 8-bit
+// integers, one power of two for every 32 neighbours of a row): loads and stores of eight
+// neighbouring floats of any type, the decoders, the activation functions.
+#pragma once
+#include "lp_device.h"
+
+namespace lp {
+
+constexpr int kMx4Group = 256; // mx4 rows are padded to whole groups of this many elements
+
+static inline size_t mx4_blocks(size_t cols) { return (cols + kMx4Group - 1) / kMx4Group * (kMx4Group / 32); }
+static inline size_t ckpt8_blocks(size_t cols) { return (cols + 31) / 32; }
+
+inline size_t dtype_size(lp_dtype t) { return t == LP_F32 ? 4 : 2; }
+inline bool dtype_ok(lp_dtype t) { return (int)t >= 0 && (int)t <= 2; }
+inline bool actfn_ok(lp_actfn f) { return (int)f >= 0 && (int)f <= 3; }
+inline bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// x / d and x % d for 0 <= x < 2^31 with m = floor(2^32 / d) (d = 1: 2^32 - 1) from the host
+__device__ __forceinline__ void piece_place(unsigned x, unsigned d, unsigned m, unsigned &q, unsigned &r)
+{
+    q = __umulhi(x, m);
+    r = x - q * d;
+    if (r >= d) {
+        ++q;
+        r -= d;
+    }
+}
+inline unsigned piece_magic(unsigned d) { return d <= 1 ? 0xffffffffu : (unsigned)((1ull << 32) / d); }
+
+// ------------------------------------------------------------------ eight neighbouring floats
+
+typedef float v8f __attribute__((ext_vector_type(8)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+
+// One load or store of the whole vector at the element's own alignment (the memory system takes 16 bytes at
+// any address), or element by element where fewer than eight exist.
+template <typename T>
+__device__ __forceinline__ v8f load8(const T *p, int n)
+{
+    typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    v8f v = 0.0f;
+    if (n >= 8) {
+        const V t = *reinterpret_cast<const V *>(p);
+        v = __builtin_convertvector(t, v8f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < n) v[j] = (float)p[j];
+    }
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int n, v8f v)
+{
+    typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    const V t = __builtin_convertvector(v, V);
+    if (n >= 8) {
+        *reinterpret_cast<V *>(p) = t;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 7; ++j)
+            if (j < n) p[j] = t[j];
+    }
+}
+
+// ---------------------------------------------------------------------------------- decoders
+
+__device__ __forceinline__ float power_of_byte(int e) { return __uint_as_float((unsigned)e << 23); } // 2^(e - 127), 1 <= e <= 254
+
+// eight mx4 elements (one word of codes) times 2^(e - 127)
+__device__ __forceinline__ v8f mx4_values(unsigned w, int e)
+{
+    const float s = power_of_byte(e);
+    const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+    const v2f c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
+    return v8f{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+
+// eight ckpt8 elements (two words of codes) times 2^(e - 133)
+__device__ __forceinline__ v8f ckpt8_values(v2u w, int e)
+{
+    const float s = power_of_byte(e - 6);
+    v8f v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)(signed char)(w[j >> 2] >> (8 * (j & 3))) * s;
+    return v;
+}
+
+// ----------------------------------------------------------------------- activation functions
+
+// 1 / (1 + exp(-z)): the hardware's 2^x and reciprocal, each within one unit in the last place of 32 bits.
+// exp overflows to infinity for z < -88 and the reciprocal of that is 0.
+__device__ __forceinline__ float logistic(float z)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * z));
+}
+
+constexpr float kGelu2C = 1.59576912160573071176f;   // 2 sqrt(2 / pi)
+constexpr float kGeluA = 0.044715f;
+
+// the functions' factor that multiplies h; -Inf is taken as a number far out, where the product is a (signed) zero
+__device__ __forceinline__ float act_value(float h, lp_actfn f)
+{
+    if (f == LP_ACT_RELU) return h < 0.0f ? 0.0f : h;
+    const float g = h < -1e30f ? -1e30f : h;
+    if (f == LP_ACT_SILU) return g * logistic(g);
+    if (f == LP_ACT_GELU_TANH) return g * logistic(kGelu2C * (g + kGeluA * g * g * g));
+    return h;
+}
+
+// d act / dh.  Beyond 30 in magnitude the slopes are 0 or 1 to all 32 bits, and the powers stay finite.
+__device__ __forceinline__ float act_slope(float h, lp_actfn f)
+{
+    if (f == LP_ACT_RELU) return h > 0.0f ? 1.0f : 0.0f;
+    if (f == LP_ACT_SILU) {
+        const float g = fminf(fmaxf(h, -100.0f), 100.0f), s = logistic(g);
+        return s * (1.0f + g * (1.0f - s));
+    }
+    if (f == LP_ACT_GELU_TANH) {
+        const float g = fminf(fmaxf(h, -30.0f), 30.0f), q = g * g;
+        const float s = logistic(kGelu2C * g * (1.0f + kGeluA * q));
+        return s * (1.0f + g * (1.0f - s) * kGelu2C * (1.0f + 3.0f * kGeluA * q));
+    }
+    return 1.0f;
+}
+
+// --------------------------------------------------------------- as called by the products' file
+
+// brings rows x cols floats to mx4, nearest even (no arguments left to check)
+void mx4_quantize_launch(const void *x, lp_dtype xt, size_t rows, size_t cols, size_t ldx, void *codes, void *scales, hipStream_t st);
+
+} // namespace lp

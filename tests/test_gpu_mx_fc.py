@@ -1,0 +1,329 @@
+"""The microscaled inner products and their gradients against plain 64-bit products, through the C ABI.  A result may be off by
+what sums in 32 bits may be off in any order (mx_helpers.product_error) and by its own rounding."""
+import numpy as np
+import pytest
+import torch
+
+import mx_helpers as mx
+import paper_1711_04713_amd as lp
+from test_gpu_mx import ACTS, ckpt8_buffers, junk_is_left, mx4_buffers, strided
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+# M, K, Nout: one of each; one row; a few; ragged against every tile; whole tiles; long reductions; many rows
+SIZES = [(1, 1, 1), (1, 4096, 512), (2, 300, 33), (5, 1024, 1000), (16, 512, 256), (17, 513, 257), (37, 2500, 1001), (64, 256, 130),
+         (130, 100, 70), (255, 777, 129), (256, 1024, 512), (300, 1100, 600), (513, 260, 1025), (1030, 64, 31), (3, 25088, 65),
+         (200, 9000, 96), (2100, 512, 40), (128, 8192, 1111)]
+
+
+def weights(n, k, seed, spread=8):
+    """An mx4 tensor of random codes and scales, and its values in 64 bits."""
+    g = torch.Generator().manual_seed(seed)
+    blocks = mx.mx4_blocks(k)
+    codes = torch.randint(0, 256, (n, blocks * 16), generator=g).to(torch.uint8)
+    code = torch.arange(blocks * 16).reshape(1, -1)
+    codes = torch.where(2 * code >= k, 0, torch.where(2 * code + 1 >= k, codes & 15, codes)).to(torch.uint8)   # padding
+    scales = torch.randint(127 - spread, 127 + spread, (n, blocks), generator=g).to(torch.uint8)
+    return codes.cuda(), scales.cuda(), torch.from_numpy(mx.mx4_values(codes, scales, k)).cuda()
+
+
+def inputs(m, k, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn((m, k), generator=g) * torch.exp(torch.randn(k, generator=g))).to(dtype)
+
+
+def workspace(size):
+    return torch.full((size,), 0xA5, dtype=torch.uint8, device="cuda") if size else None
+
+
+def product(a, b):
+    """a [I][C] @ b [C][J] in 64 bits, and the same of magnitudes (dense operands)."""
+    a, b = a.double().contiguous(), b.double().contiguous()
+    return torch.mm(a, b).cpu().numpy(), torch.mm(a.abs(), b.abs()).cpu().numpy()
+
+
+def run_fwd(m, k, n, x, w, y, bias=None, act="none", x_scales=None):
+    lp.lp_mx4_fc_fwd(m, k, n, x, w[0], w[1], y, x_scales=x_scales, bias=bias, act=ACTS[act], workspace=workspace(lp.lp_mx4_fc_workspace_bytes(m, k, n)))
+
+
+def check_fwd(m, k, n, dtype, act, with_bias, extra=-1, yt=None):
+    yt = yt or dtype
+    x = inputs(m, k, dtype, m + k)
+    w = weights(n, k, n + k)
+    bias = torch.randn(n, generator=torch.Generator().manual_seed(n)) if with_bias else None
+    xq = mx.mx4_values(*mx.mx4_quantize(x.double().numpy())[:2], k)
+    h, size = product(torch.from_numpy(xq).cuda(), w[2].t())
+    if with_bias:
+        h, size = h + bias.double().numpy(), size + np.abs(bias.double().numpy())
+    want, z = mx.act(h, act)
+    # both functions' slopes are below 1.2
+    error = 1.2 * mx.product_error(size, k + 1) + mx.act_error(want, z)
+    xd, _ = strided(x, extra)
+    y, wide = strided(torch.full((m, n), 5.0, dtype=yt), extra)
+    run_fwd(m, k, n, xd, w, y, None if bias is None else bias.cuda(), act)
+    mx.close(y, want, error, yt)
+    junk_is_left(wide, n)
+    # the same from codes that were made beforehand: the same bits
+    codes, scales = mx4_buffers(m, k)
+    lp.lp_mx4_quantize(xd, codes, scales)
+    y2 = torch.full((m, n), 5.0, dtype=yt, device="cuda")
+    run_fwd(m, k, n, codes, w, y2, None if bias is None else bias.cuda(), act, x_scales=scales)
+    assert torch.equal(y2, y)
+
+
+@pytest.mark.parametrize("size", SIZES)
+def test_forward(size):
+    check_fwd(*size, torch.bfloat16, "none", False)
+    check_fwd(*size, torch.float32, "relu", True, extra=3)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("size", [(1, 700, 129), (20, 513, 300), (150, 300, 260)])
+def test_forward_types_and_functions(size, act, dtype):
+    check_fwd(*size, dtype, act, act != "relu", extra=5)
+    check_fwd(*size, dtype, act, act == "relu", yt=torch.float32 if dtype != torch.float32 else torch.bfloat16)
+
+
+@pytest.mark.parametrize("size", [(1, 512, 64), (40, 600, 200), (260, 512, 300)])
+def test_forward_takes_the_whole_range_of_scales(size):
+    """Blocks of very small and very large scales beside each other: products far apart."""
+    m, k, n = size
+    g = torch.Generator().manual_seed(k)
+    x = torch.randn((m, k), generator=g) * torch.exp2(torch.randint(-120, 50, (m, (k + 31) // 32), generator=g).float()).repeat_interleave(32, 1)[:, :k]
+    w = weights(n, k, 3, spread=60)
+    xq = mx.mx4_values(*mx.mx4_quantize(x.double().numpy())[:2], k)
+    want, size_ = product(torch.from_numpy(xq).cuda(), w[2].t())
+    y = torch.empty((m, n), device="cuda")
+    run_fwd(m, k, n, x.cuda(), w, y)
+    mx.close(y, want, mx.product_error(size_, k), torch.float32)
+
+
+def test_forward_of_nothing_but_zeros_nan_and_infinity():
+    m, k, n = 33, 300, 70
+    w = weights(n, k, 1)
+    y = torch.empty((m, n), device="cuda")
+    for fill in (0.0, float("nan")):                              # NaN is taken as 0, like everywhere in the library
+        run_fwd(m, k, n, torch.full((m, k), fill, device="cuda"), w, y, torch.arange(n, device="cuda").float())
+        assert torch.equal(y, torch.arange(n, device="cuda").float().expand(m, n))
+    x = torch.zeros((m, k))
+    x[3, 40], x[3, 41] = float("inf"), 1.5                        # saturates at 6 times the block's scale: 2^(0 - 2)
+    run_fwd(m, k, n, x.cuda(), w, y)
+    want = torch.zeros((m, n), dtype=torch.double)
+    want[3] = (w[2][:, 40] * 1.5 + w[2][:, 41] * 1.5).cpu()
+    assert torch.equal(y.cpu().double(), want)
+
+
+def check_dgrad(m, k, n, dxt, extra=-1):
+    dy = inputs(m, n, torch.bfloat16, m + n)
+    w = weights(n, k, n + 2 * k)
+    want, size = product(dy.cuda(), w[2])
+    d, _ = strided(dy, extra)
+    dx, wide = strided(torch.full((m, k), 5.0, dtype=dxt), extra)
+    lp.lp_mx4_fc_dgrad(m, k, n, d, w[0], w[1], dx, workspace=workspace(lp.lp_mx4_fc_dgrad_workspace_bytes(m, k, n)))
+    mx.close(dx, want, mx.product_error(size, n), dxt)
+    junk_is_left(wide, k)
+
+
+@pytest.mark.parametrize("size", SIZES)
+def test_input_gradient(size):
+    check_dgrad(*size, torch.float32)
+    check_dgrad(*size, torch.bfloat16, extra=3)
+    check_dgrad(*size, torch.bfloat16, extra=8)
+
+
+def kept(m, k, seed):
+    x = inputs(m, k, torch.float32, seed)
+    codes, scales = mx.ckpt8_quantize(x.double().numpy())
+    return (torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), torch.from_numpy(mx.ckpt8_values(codes, scales, k)).cuda())
+
+
+def check_wgrad(m, k, n, dwt, with_bias, accumulate=False, extra=-1):
+    dy = inputs(m, n, torch.bfloat16, m + n)
+    x = kept(m, k, m + k) if m else (*ckpt8_buffers(0, k), torch.zeros((0, k), device="cuda").double())
+    want, size = product(dy.cuda().t(), x[2])
+    d, _ = strided(dy, extra)
+    before = torch.randn((n, k), generator=torch.Generator().manual_seed(1)).to(dwt) if accumulate else torch.full((n, k), 5.0, dtype=dwt)
+    dw, wide = strided(before, extra)
+    db = torch.ones(n, device="cuda") if with_bias else None
+    lp.lp_ckpt8_fc_wgrad(m, k, n, d, x[0], x[1], dw, dbias=db, accumulate=accumulate,
+                         workspace=workspace(lp.lp_ckpt8_fc_wgrad_workspace_bytes(m, k, n)))
+    if accumulate:
+        want, size = want + before.double().numpy(), size + before.double().abs().numpy()
+    mx.close(dw, want, mx.product_error(size, m + 1), dwt)
+    if with_bias:
+        mx.close(db, dy.double().sum(0).numpy() + accumulate, mx.product_error(dy.double().abs().sum(0).numpy() + accumulate, m + 1), torch.float32)
+    junk_is_left(wide, k)
+
+
+@pytest.mark.parametrize("size", SIZES + [(0, 70, 40), (4000, 200, 136)])
+def test_weight_gradient(size):
+    check_wgrad(*size, torch.float32, True)
+    check_wgrad(*size, torch.bfloat16, True, accumulate=True, extra=3)
+    check_wgrad(*size, torch.float32, False, accumulate=True, extra=8)
+
+
+def test_gradients_against_differences():
+    """The product is linear in its input's values and in the weights' values: with 4-bit inputs that are exact, differences of the
+    forward call give the gradients of sum(dY * Y)."""
+    m, k, n = 5, 96, 40
+    g = torch.Generator().manual_seed(2)
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0])
+    x = grid[torch.randint(0, 6, (m, k), generator=g)] * torch.sign(torch.randn((m, k), generator=g))
+    x[:, ::32] = 6.0                                               # holds every block's scale where it is
+    w = weights(n, k, 7, spread=1)
+    dy = torch.randn((m, n), generator=g).bfloat16()
+    loss = lambda v: float((run(v).cpu().double() * dy.double()).sum())  # noqa: E731
+
+    def run(v):
+        y = torch.empty((m, n), device="cuda")
+        run_fwd(m, k, n, v.cuda(), w, y)
+        return y
+
+    dx = torch.empty((m, k), device="cuda")
+    lp.lp_mx4_fc_dgrad(m, k, n, dy.cuda(), w[0], w[1], dx, workspace=workspace(lp.lp_mx4_fc_dgrad_workspace_bytes(m, k, n)))
+    dw = torch.empty((n, k), device="cuda")
+    codes, scales = ckpt8_buffers(m, k)
+    lp.lp_ckpt8_save(x.cuda(), codes, scales)
+    lp.lp_ckpt8_fc_wgrad(m, k, n, dy.cuda(), codes, scales, dw, workspace=workspace(lp.lp_ckpt8_fc_wgrad_workspace_bytes(m, k, n)))
+    base, size = loss(x), float((dy.double().abs() @ w[2].cpu().abs()).max()) * 6
+    for i, j in ((0, 1), (2, 33), (4, 95), (3, 50)):
+        v = x.clone()
+        v[i, j] = 6.0                                             # (no element there is 6 before)
+        want = (loss(v) - base) / float(v[i, j] - x[i, j])
+        assert abs(want - float(dx[i, j])) < 1e-4 * size
+    # dW . W = sum(dY * Y) (Euler, the product is homogeneous of degree one in W)
+    assert abs(float((dw.cpu().double() * w[2].cpu()).sum()) - base) < 1e-5 * float((dw.cpu().double() * w[2].cpu()).abs().sum())
+
+
+def test_no_rows():
+    w = weights(40, 70, 1)
+    assert lp.lp_mx4_fc_workspace_bytes(0, 70, 40) == 0
+    lp.lp_mx4_fc_fwd(0, 70, 40, torch.empty((0, 70), device="cuda"), w[0], w[1], torch.empty((0, 40), device="cuda"))
+    lp.lp_mx4_fc_dgrad(0, 70, 40, torch.empty((0, 40), dtype=torch.bfloat16, device="cuda"), w[0], w[1], torch.empty((0, 70), device="cuda"))
+
+
+@pytest.mark.parametrize("size", [(1, 4096, 640), (40, 9000, 300), (700, 520, 260)])
+def test_equal_calls_give_equal_bits(size):
+    m, k, n = size
+    x, w, dy = inputs(m, k, torch.bfloat16, 1).cuda(), weights(n, k, 2), inputs(m, n, torch.bfloat16, 3).cuda()
+    c = kept(m, k, 4)
+    out = []
+    for _ in range(3):
+        y, dx, dw, db = (torch.empty(s, device="cuda") for s in ((m, n), (m, k), (n, k), (n,)))
+        run_fwd(m, k, n, x, w, y)
+        lp.lp_mx4_fc_dgrad(m, k, n, dy, w[0], w[1], dx, workspace=workspace(lp.lp_mx4_fc_dgrad_workspace_bytes(m, k, n)))
+        lp.lp_ckpt8_fc_wgrad(m, k, n, dy, c[0], c[1], dw, dbias=db, workspace=workspace(lp.lp_ckpt8_fc_wgrad_workspace_bytes(m, k, n)))
+        out.append((y, dx, dw, db))
+    for other in out[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(out[0], other))
+
+
+class Layer:
+    """A linear layer with an activation function trained on mx4 weights: what a program that uses the calls together keeps."""
+
+    def __init__(self, m, k, n, act, seed):
+        self.m, self.k, self.n, self.act = m, k, n, ACTS[act]
+        self.name = act
+        g = torch.Generator().manual_seed(seed)
+        self.master = (torch.randn((n, k), generator=g) / k ** 0.5).cuda()
+        self.bias = torch.randn(n, generator=g).cuda() * 0.1
+        self.w = mx4_buffers(n, k)
+        self.kept_in, self.kept_h = ckpt8_buffers(m, k), ckpt8_buffers(m, n)
+        bf = dict(dtype=torch.bfloat16, device="cuda")
+        self.h, self.y, self.dh, self.dx = torch.empty((m, n), **bf), torch.empty((m, n), **bf), torch.empty((m, n), **bf), torch.empty((m, k), **bf)
+        self.dw, self.db = torch.empty((n, k), device="cuda"), torch.empty(n, device="cuda")
+        size = max(f(m, k, n) for f in (lp.lp_mx4_fc_workspace_bytes, lp.lp_mx4_fc_dgrad_workspace_bytes, lp.lp_ckpt8_fc_wgrad_workspace_bytes))
+        self.ws = torch.empty(max(size, 16), dtype=torch.uint8, device="cuda")
+
+    def forward(self, x):
+        lp.lp_mx4_quantize(self.master, *self.w)
+        lp.lp_ckpt8_save(x, *self.kept_in)
+        lp.lp_mx4_fc_fwd(self.m, self.k, self.n, x, *self.w, self.h, bias=self.bias, workspace=self.ws)
+        lp.lp_ckpt8_save(self.h, *self.kept_h, act=self.act, y=self.y)
+        return self.y
+
+    def backward(self, dy):
+        lp.lp_ckpt8_act_bwd(*self.kept_h, dy, self.dh, self.act)
+        lp.lp_ckpt8_fc_wgrad(self.m, self.k, self.n, self.dh, *self.kept_in, self.dw, dbias=self.db, workspace=self.ws)
+        lp.lp_mx4_fc_dgrad(self.m, self.k, self.n, self.dh, *self.w, self.dx, workspace=self.ws)
+        return self.dx
+
+
+def test_two_layers_forward_and_backward_eagerly_and_from_a_graph():
+    m, sizes = 70, (200, 333, 90)
+    layers = [Layer(m, sizes[0], sizes[1], "gelu", 1), Layer(m, sizes[1], sizes[2], "silu", 2)]
+    x, dy = inputs(m, sizes[0], torch.bfloat16, 3).cuda(), (inputs(m, sizes[2], torch.bfloat16, 4) * 0.1).cuda()
+
+    def step():
+        y = layers[1].forward(layers[0].forward(x))
+        layers[0].backward(layers[1].backward(dy))
+        return y
+
+    step()
+    torch.cuda.synchronize()
+    outs = lambda: [layers[1].y] + [t for l in layers for t in (l.dw, l.db, l.dx)]  # noqa: E731
+    eager = [t.clone() for t in outs()]
+    # each call from the tensors that it was given, in 64 bits
+    a = x
+    for l in layers:
+        w = torch.from_numpy(mx.mx4_values(*mx.mx4_quantize(l.master.cpu().double().numpy())[:2], l.k)).cuda()
+        aq = torch.from_numpy(mx.mx4_values(*mx.mx4_quantize(a.cpu().double().numpy())[:2], l.k)).cuda()
+        h, size = product(aq, w.t())
+        b = l.bias.cpu().double().numpy()
+        mx.close(l.h, h + b, mx.product_error(size + np.abs(b), l.k + 1), torch.bfloat16)
+        y, z = mx.act(l.h.cpu().double().numpy(), l.name)
+        mx.close(l.y, y, mx.act_error(y, z), torch.bfloat16)
+        x8 = torch.from_numpy(mx.ckpt8_values(*mx.ckpt8_quantize(a.cpu().double().numpy()), l.k)).cuda()
+        dw, size = product(l.dh.t(), x8)
+        mx.close(l.dw, dw, mx.product_error(size, m), torch.float32)
+        dx, size = product(l.dh, w)
+        mx.close(l.dx, dx, mx.product_error(size, l.n), torch.bfloat16)
+        a = l.y
+    # captured and replayed, with other work in between and other inputs in one replay
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    kept_x = x.clone()
+    for other in (False, True, False, False):
+        for t in outs():
+            t.zero_()
+        x.copy_(kept_x * 2 if other else kept_x)
+        graph.replay()
+        torch.cuda.synchronize()
+        same = [torch.equal(p, q) for p, q in zip(outs(), eager)]
+        assert all(same) == (not other)
+        _ = torch.randn((300, 300), device="cuda") @ torch.randn((300, 300), device="cuda")
+        if other:
+            got = [t.clone() for t in outs()]
+            step()
+            assert all(torch.equal(p, q) for p, q in zip(outs(), got))
+        torch.cuda.synchronize()
+
+
+def test_calls_on_two_streams_with_workspaces_of_their_own():
+    m, k, n = 120, 5000, 200
+    w = weights(n, k, 1)
+    xs = [inputs(m, k, torch.bfloat16, s).cuda() for s in (1, 2)]
+    want = []
+    for x in xs:
+        y = torch.empty((m, n), device="cuda")
+        run_fwd(m, k, n, x, w, y)
+        want.append(y)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    ws = [workspace(lp.lp_mx4_fc_workspace_bytes(m, k, n)) for _ in xs]
+    ys = [torch.empty((m, n), device="cuda") for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, x, y, v in zip(streams, xs, ys, ws):
+            with torch.cuda.stream(s):
+                lp.lp_mx4_fc_fwd(m, k, n, x, w[0], w[1], y, workspace=v)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, ys))
