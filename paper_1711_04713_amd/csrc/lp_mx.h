@@ -109,6 +109,15 @@ __device__ __forceinline__ float act_value(float h, lp_actfn f)
     return h;
 }
 
+__device__ __forceinline__ v8f act_values(v8f v, lp_actfn f)
+{
+    if (f != LP_ACT_NONE) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = act_value(v[j], f);
+    }
+    return v;
+}
+
 // d act / dh.  Beyond 30 in magnitude the slopes are 0 or 1 to all 32 bits, and the powers stay finite.
 __device__ __forceinline__ float act_slope(float h, lp_actfn f)
 {

@@ -169,9 +169,7 @@ __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const T *x, size_t
     codes[p] = w;
     if ((p & 3) == 0) scales[p >> 2] = (unsigned char)e;
     if (y) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = act_value(v[j], act);
-        store8(y + row * ldy + col, n, v);
+        store8(y + row * ldy + col, n, act_values(v, act));
     }
 }
 
