@@ -336,7 +336,7 @@ lp_status lp_maxpool2x2(const void *x_codes_dev, void *y_codes_dev, int N, int H
  *
  * Float tensors (x, y, dy, dx, dw) are row-major with their own row stride ld >= columns, in elements; they
  * and the bias need the alignment of their type only.  Codes are aligned to 16 bytes, mx4 scales to 8, ckpt8
- * scales not at all.  Columns beyond a row's last are neither read nor written.  No tensor may
+ * scales not at all.  What lies between a row's last column and the next row is neither used nor written.  No tensor may
  * overlap another one of the call unless its text says so.  Calls without rows do
  * nothing and return LP_OK.
  */
@@ -375,7 +375,7 @@ lp_status lp_mx4_dequantize(const void *codes_dev, const void *scales_dev, size_
  * Products and sums are held in 32 bits and rounded once.  The order of the sums depends on
  * M, K and Nout alone: equal calls give equal bits.  The workspace (lp_mx4_fc_workspace_bytes, may be 0; then it may be
  * null) needs no initialisation and carries nothing from call to call; calls that share one must not
- * overlap in time.  LP_EUNSUPPORTED: M, K or Nout above 2^24.
+ * overlap in time.  LP_EUNSUPPORTED: M, K or Nout above 2^24, or two of them with a product of 2^40 or more.
  */
 lp_status lp_mx4_fc_workspace_bytes(int M, int K, int Nout, size_t *bytes_host);
 lp_status lp_mx4_fc_fwd(int M, int K, int Nout, const void *x_dev, lp_dtype xt, size_t ldx, const void *x_scales_dev,

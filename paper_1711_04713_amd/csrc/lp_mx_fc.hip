@@ -27,33 +27,104 @@ __device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t from, unsigned 
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (LdsPtr)to, 4, lane_offset, offset, 0, 0);
 }
 
+// everything that this wave has asked for has arrived, and so it is in every other wave of the workgroup
+__device__ __forceinline__ void all_arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // -------------------------------------------------------------------------------- results
 
 // Where a product's sums go: out[i][j] = act(sum + bias[j]), rounded once.  A product that is cut along its reduction
 // writes 32-bit sums of its parts to the workspace in the same way (no bias, no function), part p `part` elements further.
+// accumulate: what is there is added before the rounding.
 struct Sink {
     void *y;
     size_t ld, part;
     const float *bias;
     lp_actfn act;
+    int accumulate;
 };
+
+// Eight neighbouring results of a row, n of which exist.
+template <typename T>
+__device__ __forceinline__ void put8(const Sink &s, T *to, const float *bias, int n, v8f v)
+{
+    if (s.bias) v += load8(bias, n);
+    if (s.accumulate) v += load8(to, n);
+    store8(to, n, act_values(v, s.act));
+}
+
+// A wave's results, MB x NB blocks of 32 rows x 32 columns from (i0, j0) on: 32 rows at a time through a piece of LDS of its
+// own, so that they leave as whole rows, eight neighbours a lane.  In the accumulators a lane holds, of row lane % 32 of a
+// block, columns 8 g + 4 (lane / 32) + 0..3 in registers 4 g ..
+constexpr int result_row(int NB) { return NB * 32 + 4; } // floats, padded
+constexpr int result_bytes(int NB) { return 32 * result_row(NB) * 4; }
+template <int MB, int NB, typename T>
+__device__ __forceinline__ void put_results(const Sink &out, int part, float *mine, const v16f (&acc)[NB][MB], int i0, int j0, int I, int J)
+{
+    constexpr int ROW = result_row(NB);
+    const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    T *y = (T *)out.y + part * out.part;
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+        const int ib = i0 + b * 32;
+        if (ib >= I) break;
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const v16f &c = acc[j][b];
+                *(v4f *)(mine + l32 * ROW + j * 32 + 8 * g + 4 * h) = v4f{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (one wave: its own writes are all there)
+#pragma unroll 2
+        for (int q = 0; q < 2 * NB; ++q) {
+            const int k = q * 64 + lane, row = k / (NB * 4), col = k % (NB * 4) * 8;
+            const v4f lo = *(const v4f *)(mine + row * ROW + col), hi = *(const v4f *)(mine + row * ROW + col + 4);
+            const int i = ib + row, j = j0 + col;
+            if (i < I && j < J) put8(out, y + i * out.ld + j, out.bias + j, J - j, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+}
+
+// Which tile a workgroup computes: consecutive workgroups go round the dies, each die has a run of consecutive items; an item
+// is a part of the reduction and a tile, row tiles walked kTileGroup at a time: 32 workgroups of a die share 4 x 8 tiles.
+constexpr int kTileGroup = 4;
+struct Grid {
+    int tiles_i, tiles_j, stages, stages_per_part, parts, work, per_xcd;
+};
+struct Place {
+    int part, tile_i, tile_j, first, last; // stages first .. last - 1
+};
+__device__ __forceinline__ bool find_place(const Grid &g, Place *p)
+{
+    const int item = (blockIdx.x % kXCDs) * g.per_xcd + blockIdx.x / kXCDs;
+    if (item >= g.work) return false;
+    // (divisions run on the vector unit: what comes back is said to be the same in all lanes)
+    const int tiles = g.tiles_i * g.tiles_j;
+    p->part = __builtin_amdgcn_readfirstlane(item / tiles);
+    const int tile = item - p->part * tiles, group = __builtin_amdgcn_readfirstlane(tile / (kTileGroup * g.tiles_j));
+    const int in_group = tile - group * kTileGroup * g.tiles_j, rows = min(kTileGroup, g.tiles_i - group * kTileGroup);
+    p->tile_j = __builtin_amdgcn_readfirstlane(in_group / rows);
+    p->tile_i = group * kTileGroup + in_group - p->tile_j * rows;
+    p->first = p->part * g.stages_per_part;
+    p->last = min(g.stages, p->first + g.stages_per_part);
+    return true;
+}
 
 // y = act(sum of the parts + bias): a thread takes eight neighbours of a row
 template <typename T>
-__global__ __launch_bounds__(256) void join_parts_kernel(const float *__restrict__ parts, int count, size_t part, size_t ldp, T *__restrict__ y, size_t ldy,
-                                                         int I, int J, unsigned per_row, unsigned magic, unsigned total, const float *__restrict__ bias,
-                                                         lp_actfn act)
+__global__ __launch_bounds__(256) void join_parts_kernel(const float *__restrict__ parts, int count, size_t part, size_t ldp, Sink out, int J, unsigned per_row,
+                                                         unsigned magic, unsigned total)
 {
     const unsigned p = blockIdx.x * 256 + threadIdx.x;
     if (p >= total) return;
     unsigned row, piece;
     piece_place(p, per_row, magic, row, piece);
-    const int j = 8 * (int)piece, n = min(J - j, 8);
+    const int j = 8 * (int)piece;
     const float *q = parts + row * ldp + j; // (rows of the parts are whole pieces)
     v8f v = load8(q, 8);
     for (int k = 1; k < count; ++k) v += load8(q + k * part, 8);
-    if (bias) v += load8(bias + j, n);
-    store8(y + row * ldy + j, n, act_values(v, act));
+    put8(out, (T *)out.y + row * out.ld + j, out.bias + j, J - j, v);
 }
 
 // ------------------------------------------------------------------------------- mx4 times mx4
@@ -73,11 +144,10 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float *__restrict
 // Weights are the row operand: a lane ends up with four neighbouring columns of one row of y.
 struct Mx4Args {
     const unsigned char *xc, *xs, *wc, *ws;
-    int M, N, blocks, stages, stages_per_part, tiles_m, tiles_n, parts, work, per_xcd; // stages_per_part: a multiple of 4
+    int M, N, blocks;
+    Grid grid; // stages_per_part: a multiple of 4
     Sink out;
 };
-
-constexpr int kTileGroup = 4; // row tiles that are walked together: 32 workgroups of a die share 4 x 8 tiles
 
 template <int MB, int NB, int WM, int WN, typename OutT>
 __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Args a)
@@ -85,20 +155,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
     constexpr int TM = MB * 32 * WM, TN = NB * 32 * WN, WAVES = WM * WN, ROWS = TM + TN, STAGE = ROWS * 128, PER = ROWS / 8 / WAVES;
     constexpr int SROWS = ROWS / WAVES, SPER = SROWS / 32; // rows whose scale bytes a wave brings, loads that takes
     static_assert(TM % SROWS == 0, "of one tensor");
-    constexpr int OUTROW = NB * 32 + 4; // a wave's row of results in LDS, floats, padded
-    constexpr int OUTWAVE = 32 * OUTROW * 4;
     // (the scale bytes of a row's stages that do not exist are read too, from whatever follows: 32 bytes more)
     __shared__ __align__(1024) unsigned char lds[2 * STAGE + ROWS * 32 + 32];
-    static_assert(WAVES * OUTWAVE <= (int)sizeof(lds), "results pass through the same memory");
-    // work item: consecutive workgroups go round the dies, each die has a run of consecutive items
-    const int item = (blockIdx.x % kXCDs) * a.per_xcd + blockIdx.x / kXCDs;
-    if (item >= a.work) return;
-    // (divisions run on the vector unit: what comes back is said to be the same in all lanes)
-    const int tiles = a.tiles_m * a.tiles_n, part = __builtin_amdgcn_readfirstlane(item / tiles), tile = item - part * tiles;
-    const int group = __builtin_amdgcn_readfirstlane(tile / (kTileGroup * a.tiles_n)), in_group = tile - group * kTileGroup * a.tiles_n;
-    const int rows = min(kTileGroup, a.tiles_m - group * kTileGroup), tile_n = __builtin_amdgcn_readfirstlane(in_group / rows);
-    const int m0 = (group * kTileGroup + in_group - tile_n * rows) * TM, n0 = tile_n * TN;
-    const int first = part * a.stages_per_part, last = min(a.stages, first + a.stages_per_part);
+    static_assert(WAVES * result_bytes(NB) <= (int)sizeof(lds), "results pass through the same memory");
+    Place p;
+    if (!find_place(a.grid, &p)) return;
+    const int m0 = p.tile_i * TM, n0 = p.tile_j * TN, first = p.first, last = p.last;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, h = lane >> 5, wm = wave % WM, wn = wave / WM;
@@ -147,7 +209,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
     };
     auto load_narrow_scales = [&]() __attribute__((always_inline)) {
         const __amdgpu_buffer_rsrc_t from = scales_of(-1);
-        for (int q = 0; q < a.stages; ++q)
+        for (int q = 0; q < last; ++q)
 #pragma unroll
             for (int i = 0; i < SPER; ++i)
                 load_lds4(from, scales + q * ROWS * 8 + wave * SROWS * 8 + i * 256, row_of(wave * SROWS + i * 32 + lane / 2) * (unsigned)a.blocks + 4 * (lane & 1), 8 * q);
@@ -204,8 +266,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
         LP_STEP(Q, 1, true)
         fragments(B, 3);
         LP_STEP(Q, 2, false)
-        __builtin_amdgcn_s_waitcnt(0);
-        __builtin_amdgcn_s_barrier();
+        all_arrived();
         fragments(B ^ 1, 0);
         stage(t + 2, B, L0, L1);
         if (Q == 0) load_scales(t + 4);
@@ -215,8 +276,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
     if (narrow) load_narrow_scales();
     else load_scales(first);
     stage(first, 0, L0, L3);
-    __builtin_amdgcn_s_waitcnt(0);
-    __builtin_amdgcn_s_barrier();
+    all_arrived();
     stage(first + 1, 1, L0, L1);
     fragments(0, 0);
     for (int t = first;; t += 4) {
@@ -230,178 +290,332 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
         whole_stage(t + 3, std::integral_constant<int, 3>());
         if (t + 4 >= last) break;
     }
-    __builtin_amdgcn_s_waitcnt(0);
-    __builtin_amdgcn_s_barrier();
-    // Results: 32 rows at a time through the wave's own piece of LDS, so that they leave as whole rows, eight neighbours a lane.
-    float *mine = (float *)(lds + wave * OUTWAVE);
-    OutT *y = (OutT *)a.out.y + part * a.out.part;
-    const int nw = n0 + wn * NB * 32;
-#pragma unroll
-    for (int i = 0; i < MB; ++i) {
-        const int mw = m0 + (wm * MB + i) * 32;
-        if (mw >= a.M) break;
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const v16f &c = acc[j][i];
-                *(v4f *)(mine + l32 * OUTROW + j * 32 + 8 * g + 4 * h) = v4f{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
-            }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll 2
-        for (int q = 0; q < 2 * NB; ++q) {
-            const int k = q * 64 + lane, row = k / (NB * 4), col = k % (NB * 4) * 8;
-            const v4f lo = *(const v4f *)(mine + row * OUTROW + col), hi = *(const v4f *)(mine + row * OUTROW + col + 4);
-            v8f v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            const int m = mw + row, n = nw + col;
-            if (m < a.M && n < a.N) {
-                if (a.out.bias) v += load8(a.out.bias + n, a.N - n);
-                store8(y + m * a.out.ld + n, a.N - n, act_values(v, a.out.act));
-            }
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
+    all_arrived();
+    put_results<MB, NB, OutT>(a.out, p.part, (float *)(lds + wave * result_bytes(NB)), acc, m0 + wm * MB * 32, n0 + wn * NB * 32, a.M, a.N);
 }
 
 // -------------------------------------------------------------------------------- gradients
 
-constexpr int PT = 64;  // rows and columns of a tile
-constexpr int PC = 16;  // positions of the reduction per step
-
-struct Mx4Rows { // element (row, pos) of an mx4 tensor
+// D[i][j] = sum_c A(i, c) B(c, j) on v_mfma_f32_32x32x16_bf16, A the bfloat16 gradient dY, B an mx4 or ckpt8 tensor whose rows are
+// the reduction.  Values of either format have at most seven significant bits: they are exact in bfloat16.
+//   gradient of the input:    i = m, c = n, j = k; A(i, c) = dY[i][c], B = Wq
+//   gradient of the weights:  i = n, c = m, j = k; A(i, c) = dY[c][i], B = X8
+//
+// A workgroup owns TI x TJ results, a wave MB x NB blocks of 32 x 32; a stage is 64 positions of the reduction in one of two LDS
+// buffers.  B's codes pass through registers, a block of 32 a thread, loaded two stages ahead, decoded one stage ahead; dY
+// comes by loads to LDS (or, where its rows do not start on words, through registers like the codes).  The matrix
+// instruction wants eight neighbouring positions of a row or column in a lane: those of dY's rows lie together in memory
+// (16-byte piece p of row r at place p ^ (r % 8), as above); tiles with the reduction along their rows are read by
+// ds_read_b64_tr_b16, which hands each of 16 lanes four rows' elements of its column.  Their rows are 512 (or 256) bytes, so
+// the four rows of such a read lie in the same banks unless the 64-byte pieces of row r change places with r % 4.
+//
+// B is the row operand of the instruction, so that a lane ends up with four neighbouring columns of one row of D.
+struct GradArgs {
+    const __bf16 *dy;
+    size_t ld;
     const unsigned char *codes, *scales;
-    size_t blocks;
-    __device__ float at(int row, int pos) const
-    {
-        const int code = codes[(size_t)row * blocks * 16 + (pos >> 1)] >> (4 * (pos & 1)) & 15;
-        const int e = code >> 1 & 3, m = code & 1;
-        const float v = e ? (float)((2 + m) << (e - 1)) * 0.5f : 0.5f * m;
-        return (code & 8 ? -v : v) * power_of_byte(scales[(size_t)row * blocks + (pos >> 5)]);
-    }
-};
-struct Ckpt8Rows {
-    const signed char *codes;
-    const unsigned char *scales;
-    size_t blocks;
-    __device__ float at(int row, int pos) const
-    {
-        return (float)codes[(size_t)row * blocks * 32 + pos] * power_of_byte(scales[(size_t)row * blocks + (pos >> 5)] - 6);
-    }
-};
-struct Bf16Rows {
-    const __bf16 *p;
-    size_t ld;
-    __device__ float at(int row, int pos) const { return (float)p[(size_t)row * ld + pos]; }
+    int I, J, C, blocks; // blocks of 32 in a row of B
+    Grid grid;
+    float *db;           // sums of dY over the reduction (weights only; may be null), part p at db + p * db_part
+    size_t db_part;
+    int db_accumulate;
+    Sink out;
 };
 
-struct Output {
-    void *y;
-    lp_dtype t;
-    size_t ld;
-    const float *bias;
-    lp_actfn act;
-    int accumulate;
-    __device__ void put(int i, int j, float v) const
-    {
-        const size_t at = (size_t)i * ld + j;
-        if (bias) v += bias[j];
-        if (accumulate) v += t == LP_F32 ? ((float *)y)[at] : (float)((__bf16 *)y)[at];
-        v = act_value(v, act);
-        if (t == LP_F32) ((float *)y)[at] = v;
-        else if (t == LP_BF16) ((__bf16 *)y)[at] = (__bf16)v;
-        else ((_Float16 *)y)[at] = (_Float16)v;
-    }
-};
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s *LdsV4;
 
-// A(i, c): a.at(i, c), or a.at(c, i) where the reduction runs over a's rows; B(c, j) likewise: b.at(j, c) or b.at(c, j).
-template <bool A_BY_POS, bool B_BY_POS, typename A, typename B>
-__global__ __launch_bounds__(256) void product_kernel(A a, B b, Output out, int I, int J, int C)
+// n (at most 8) bfloat16 of a row as one 16-byte piece, zeros behind them
+__device__ __forceinline__ v4u load_piece(const __bf16 *p, int n)
 {
-    __shared__ float ta[PC][PT + 1], tb[PC][PT + 1];
-    const int tiles_i = (I + PT - 1) / PT, i0 = blockIdx.x % tiles_i * PT, j0 = blockIdx.x / tiles_i * PT, ti = threadIdx.x & 15, tj = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (int c0 = 0; c0 < C; c0 += PC) {
-        for (int k = threadIdx.x; k < PC * PT; k += 256) {
-            const int ac = A_BY_POS ? k / PT : k % PC, ai = A_BY_POS ? k % PT : k / PC;
-            ta[ac][ai] = i0 + ai < I && c0 + ac < C ? (A_BY_POS ? a.at(c0 + ac, i0 + ai) : a.at(i0 + ai, c0 + ac)) : 0.0f;
-            const int bc = B_BY_POS ? k / PT : k % PC, bj = B_BY_POS ? k % PT : k / PC;
-            tb[bc][bj] = j0 + bj < J && c0 + bc < C ? (B_BY_POS ? b.at(c0 + bc, j0 + bj) : b.at(j0 + bj, c0 + bc)) : 0.0f;
-        }
-        __syncthreads();
-        for (int c = 0; c < PC; ++c)
-            for (int u = 0; u < 4; ++u)
-                for (int v = 0; v < 4; ++v) acc[u][v] += ta[c][ti + 16 * u] * tb[c][tj * 4 + v];
-        __syncthreads();
+    typedef unsigned short V __attribute__((ext_vector_type(8), aligned(2)));
+    typedef unsigned short W __attribute__((ext_vector_type(8)));
+    const unsigned short *q = reinterpret_cast<const unsigned short *>(p);
+    W v = 0;
+    if (n >= 8) {
+        v = *reinterpret_cast<const V *>(q);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < n) v[e] = q[e];
     }
-    for (int u = 0; u < 4; ++u)
-        for (int v = 0; v < 4; ++v) {
-            const int i = i0 + ti + 16 * u, j = j0 + tj * 4 + v;
-            if (i < I && j < J) out.put(i, j, acc[u][v]);
-        }
+    return __builtin_bit_cast(v4u, v);
 }
 
-// dbias[j] (+)= sum over the rows of dY
-__global__ __launch_bounds__(256) void column_sums_kernel(Bf16Rows dy, int M, int N, float *out, int accumulate)
+// A block of 32 codes with its scale byte: 16 bytes of mx4, 32 of ckpt8.
+template <bool WEIGHTS>
+struct RawBlock {
+    v4u w[WEIGHTS ? 2 : 1];
+    int e;
+    __device__ __forceinline__ void load(const GradArgs &a, int c, int block)
+    {
+        if (c < a.C && block < a.blocks) {
+            const size_t at = (size_t)c * a.blocks + block;
+            const v4u *from = reinterpret_cast<const v4u *>(a.codes) + at * (WEIGHTS ? 2 : 1);
+#pragma unroll
+            for (int k = 0; k < (WEIGHTS ? 2 : 1); ++k) w[k] = from[k];
+            e = a.scales[at];
+        } else {
+#pragma unroll
+            for (int k = 0; k < (WEIGHTS ? 2 : 1); ++k) w[k] = 0;
+            e = 127;
+        }
+    }
+    // sixteen-byte piece k of the block's values: elements 8 k .. 8 k + 7
+    __device__ __forceinline__ v4u piece(int k) const
+    {
+        if constexpr (WEIGHTS) {
+            // q + 128 in the low byte of 2^23 is the number 2^23 + 128 + q
+            const float s = power_of_byte(e - 6);
+            v4u r;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const unsigned word = w[k >> 1][(k & 1) * 2 + (d >> 1)] ^ 0x80808080u;
+                const float lo = (__uint_as_float(__builtin_amdgcn_perm(0x4B000000u, word, 0x07060500u | (2 * (d & 1)))) - 8388736.0f) * s;
+                const float hi = (__uint_as_float(__builtin_amdgcn_perm(0x4B000000u, word, 0x07060501u | (2 * (d & 1)))) - 8388736.0f) * s;
+                r[d] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); // (their low halves are zero)
+            }
+            return r;
+        } else {
+            const float s = power_of_byte(e);
+            v4u r;
+            r[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0][k], s, 0));
+            r[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0][k], s, 1));
+            r[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0][k], s, 2));
+            r[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0][k], s, 3));
+            return r;
+        }
+    }
+};
+
+template <int MB, int NB, int WM, int WN, bool WEIGHTS, bool WORDS, typename OutT>
+__global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs a)
 {
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j >= N) return;
-    float s = 0.0f;
-    for (int m = 0; m < M; ++m) s += dy.at(m, j);
-    out[j] = accumulate ? out[j] + s : s;
+    constexpr int TI = MB * 32 * WM, TJ = NB * 32 * WN, WAVES = WM * WN, THREADS = WAVES * 64;
+    constexpr int ABYTES = TI * 128, BBYTES = TJ * 128, STAGE = ABYTES + BBYTES;
+    constexpr int PER = ABYTES / 1024 / WAVES; // a wave's loads of dY per stage, and a thread's pieces
+    constexpr int AROW = WEIGHTS ? TI * 2 : 128, BROW = TJ * 2;
+    static_assert(TJ * 2 == THREADS, "a thread decodes one block of 32 per stage");
+    __shared__ __align__(1024) unsigned char lds[2 * STAGE];
+    static_assert(WAVES * result_bytes(NB) <= (int)sizeof(lds), "results pass through the same memory");
+    Place p;
+    if (!find_place(a.grid, &p)) return;
+    const int i0 = p.tile_i * TI, j0 = p.tile_j * TJ, first = p.first, last = p.last;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, h = lane >> 5, wm = wave % WM, wn = wave / WM;
+
+    // dY.  The last stage of the whole reduction comes element by element through registers where it, or a row, ends inside a
+    // piece: what lies behind must not be multiplied, not even by zero.
+    const bool ragged = last == a.grid.stages && (last * 64 != a.C || (WEIGHTS && i0 + TI > a.I));
+    const int whole = WORDS ? last - ragged : first; // stages first .. whole - 1 come by loads to LDS
+    unsigned at[PER];
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+        if constexpr (WEIGHTS) {
+            constexpr int LANES = AROW / 16; // of a row
+            const int r = (wave * PER + q) * (64 / LANES) + lane / LANES, s = lane % LANES;
+            at[q] = (unsigned)r * (unsigned)(a.ld * 2) + (((s >> 2) ^ (r & 3)) * 4 + (s & 3)) * 16;
+        } else {
+            const int r = (wave * PER + q) * 8 + lane / 8;
+            at[q] = (unsigned)min(r, a.I - 1 - i0) * (unsigned)(a.ld * 2) + ((lane & 7) ^ (r & 7)) * 16;
+        }
+    }
+    // loads FROM .. TO - 1 of a wave's share of stage t; where nothing is to come the descriptor is empty and zeros arrive
+    auto load_dy = [&](int t, int buf, auto from, auto to) __attribute__((always_inline)) {
+        if constexpr (WORDS) {
+            const int size = __builtin_amdgcn_readfirstlane(t < whole ? -1 : 0);
+            const __bf16 *base = WEIGHTS ? a.dy + (size_t)t * 64 * a.ld + i0 : a.dy + (size_t)i0 * a.ld + t * 64;
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16 *>(base), 0, size, 0x00020000);
+#pragma unroll
+            for (int q = decltype(from)::value; q < decltype(to)::value; ++q) load_lds16(rsrc, lds + buf * STAGE + (wave * PER + q) * 1024, at[q], 0);
+        }
+    };
+    v4u raw_dy[PER];
+    auto fetch_dy = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+            const int k = q * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
+            const int row = WEIGHTS ? t * 64 + r : i0 + r, col = WEIGHTS ? i0 + s * 8 : t * 64 + s * 8;
+            const int rows = WEIGHTS ? a.C : a.I, cols = WEIGHTS ? a.I : a.C;
+            raw_dy[q] = load_piece(a.dy + row * a.ld + col, row < rows && t < last ? cols - col : 0);
+        }
+    };
+    auto place_dy = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+            const int k = q * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
+            const int to = WEIGHTS ? ((s >> 2) ^ (r & 3)) * 4 + (s & 3) : s ^ (r & 7);
+            *(v4u *)(lds + buf * STAGE + r * AROW + to * 16) = raw_dy[q];
+        }
+    };
+
+    // B: thread's row of the stage and block of the row
+    RawBlock<WEIGHTS> raw;
+    const int brow = threadIdx.x / (TJ / 32), bblock = threadIdx.x % (TJ / 32);
+    unsigned char *const bplace = lds + ABYTES + brow * BROW + (bblock ^ (brow & 3)) * 64;
+    auto load_b = [&](int t) __attribute__((always_inline)) { raw.load(a, t < last ? t * 64 + brow : a.C, j0 / 32 + bblock); };
+    auto place_b = [&](int buf, int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = from; k < to; ++k) *(v4u *)(bplace + buf * STAGE + k * 16) = raw.piece(k);
+    };
+
+    v16f acc[NB][MB] = {};
+    v8s fa[2][MB], fb[2][NB];
+    // this lane's place in a read of four rows x 16 columns (x0: the tile column of its block of 32)
+    const int tr_row = 8 * h + (lane & 15) / 4, tr_col = (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+    auto tr_place = [&](int x0, int row_bytes) __attribute__((always_inline)) { return tr_row * row_bytes + ((x0 / 32) ^ (tr_row & 3)) * 64 + tr_col; };
+    int apos[MB], bpos[NB];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) apos[b] = WEIGHTS ? tr_place((wm * MB + b) * 32, AROW) : ((wm * MB + b) * 32 + l32) * 128;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) bpos[b] = ABYTES + tr_place((wn * NB + b) * 32, BROW);
+    auto tr_read = [&](int pos, int row_bytes) __attribute__((always_inline)) {
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV4)(lds + pos)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV4)(lds + pos + 4 * row_bytes));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    auto fragments = [&](int buf, int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+            if constexpr (WEIGHTS) fa[s & 1][b] = tr_read(buf * STAGE + apos[b] + s * 16 * AROW, AROW);
+            else fa[s & 1][b] = *(const v8s *)(lds + buf * STAGE + apos[b] + ((2 * s + h) ^ (l32 & 7)) * 16);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) fb[s & 1][b] = tr_read(buf * STAGE + bpos[b] + s * 16 * BROW, BROW);
+    };
+    // sums of dY: a lane's eight positions of its column of each block
+    const bool sum_dy = WEIGHTS && a.db && p.tile_j == 0 && wn == 0;
+    float db[MB] = {};
+    auto add_dy = [&](int s) __attribute__((always_inline)) {
+        if constexpr (WEIGHTS) {
+            if (sum_dy) {
+                const v2bf one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+                for (int b = 0; b < MB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        typedef short v2sh __attribute__((ext_vector_type(2)));
+                        const v2sh two = {fa[s & 1][b][2 * e], fa[s & 1][b][2 * e + 1]};
+                        db[b] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(v2bf, two), one, db[b], false);
+                    }
+            }
+        }
+    };
+#define LP_STEP(S)                                                                                                                          \
+    _Pragma("unroll") for (int j = 0; j < NB; ++j) _Pragma("unroll") for (int i = 0; i < MB; ++i) acc[j][i] =                                \
+        __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, fb[S & 1][j]), __builtin_bit_cast(v8bf, fa[S & 1][i]), acc[j][i], 0, 0, 0); \
+    _Pragma("unroll") for (int q = 0; q < MB * NB; ++q)                                                                                      \
+    {                                                                                                                                       \
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);                                                                                  \
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                                                                                  \
+    }                                                                                                                                       \
+    __builtin_amdgcn_sched_barrier(0);                                                                                                      \
+    add_dy(S);
+    constexpr std::integral_constant<int, 0> L0;
+    constexpr std::integral_constant<int, PER / 2> L1;
+    constexpr std::integral_constant<int, PER> L2;
+    // Stage t in buffer B: while it is multiplied the next one is completed in the other buffer.
+    auto whole_stage = [&](int t, auto buffer) __attribute__((always_inline)) {
+        constexpr int B = decltype(buffer)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        fragments(B, 1);
+        load_dy(t + 1, B ^ 1, L1, L2);
+        place_b(B ^ 1, 0, 2);
+        LP_STEP(0)
+        fragments(B, 2);
+        place_b(B ^ 1, 2, 4);
+        load_b(t + 2);
+        LP_STEP(1)
+        if constexpr (!WORDS) {
+            place_dy(B ^ 1);
+            fetch_dy(t + 2);
+        }
+        fragments(B, 3);
+        LP_STEP(2)
+        if (WORDS && ragged && t + 2 == last) {
+            fetch_dy(t + 1);
+            __builtin_amdgcn_s_waitcnt(0); // (and the zeros of the empty loads have arrived)
+            place_dy(B ^ 1);
+        }
+        all_arrived();
+        fragments(B ^ 1, 0);
+        load_dy(t + 2, B, L0, L1);
+        LP_STEP(3)
+    };
+    load_b(first);
+    load_dy(first, 0, L0, L2);
+    place_b(0, 0, 4);
+    load_b(first + 1);
+    if (!WORDS || whole == first) {
+        fetch_dy(first);
+        __builtin_amdgcn_s_waitcnt(0);
+        place_dy(0);
+    }
+    if constexpr (!WORDS) fetch_dy(first + 1);
+    all_arrived();
+    load_dy(first + 1, 1, L0, L1);
+    fragments(0, 0);
+    for (int t = first;; t += 2) {
+        whole_stage(t, std::integral_constant<int, 0>());
+        if (t + 1 >= last) break;
+        whole_stage(t + 1, std::integral_constant<int, 1>());
+        if (t + 2 >= last) break;
+    }
+#undef LP_STEP
+    all_arrived();
+    if (sum_dy) {
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+            const float v = db[b] + __shfl_xor(db[b], 32);
+            const int i = i0 + (wm * MB + b) * 32 + l32;
+            float *to = a.db + p.part * a.db_part + i;
+            if (h == 0 && i < a.I) *to = a.db_accumulate ? *to + v : v;
+        }
+    }
+    put_results<MB, NB, OutT>(a.out, p.part, (float *)(lds + wave * result_bytes(NB)), acc, i0 + wm * MB * 32, j0 + wn * NB * 32, a.I, a.J);
 }
 
-static dim3 product_grid(int I, int J) { return dim3((unsigned)((I + PT - 1) / PT) * (unsigned)((J + PT - 1) / PT)); }
+// ------------------------------------------------------------------------------------- plans
 
 static bool sizes_ok(int M, int K, int Nout) { return M >= 0 && K > 0 && Nout > 0; }
-static bool sizes_taken(int M, int K, int Nout) { return M <= (1 << 24) && K <= (1 << 24) && Nout <= (1 << 24); }
+static bool sizes_taken(int M, int K, int Nout)
+{
+    const long long most = 1LL << 40;
+    return M <= (1 << 24) && K <= (1 << 24) && Nout <= (1 << 24) && (long long)M * K < most && (long long)M * Nout < most && (long long)K * Nout < most;
+}
 
 static bool mx4_ok(const void *codes, const void *scales) { return codes && aligned16(codes) && scales && aligned_to(scales, 8); }
 static bool floats_ok(const void *p, lp_dtype t, size_t cols, size_t ld) { return p && aligned_to(p, dtype_size(t)) && ld >= cols; }
 
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
-struct Mx4Plan {
-    bool large;                 // tiles of 256 x 256, else 128 x 128
-    int tiles_m, tiles_n, stages, parts, stages_per_part;
-    size_t blocks, ldp;         // blocks of 32 per row; row length of the parts' sums
-    size_t codes, scales, sums; // workspace: quantized x (if the call brings floats), sums of the parts
-    size_t total() const { return codes + scales + sums; }
+// How a product I x J with `stages` stages of its reduction is cut into workgroups.
+struct Cut {
+    bool large; // tiles of 256 x 256, else 128 x 128
+    Grid grid;
+    size_t ldp, sums; // the parts' sums: row length, bytes (0: one part)
 };
 
-static Mx4Plan mx4_plan(int M, int K, int Nout)
+static Cut cut_product(int I, int J, int stages, int step, int least)
 {
-    Mx4Plan p = {};
-    p.blocks = mx4_blocks((size_t)K);
-    p.stages = (int)(p.blocks / 8);
-    const auto tiles = [&](int side) { return ((size_t)M + side - 1) / side * (((size_t)Nout + side - 1) / side); };
-    p.large = tiles(256) >= 192;
-    const int side = p.large ? 256 : 128;
-    p.tiles_m = (M + side - 1) / side;
-    p.tiles_n = (Nout + side - 1) / side;
-    p.parts = 1;
-    if (!p.large) p.parts = (int)std::min<size_t>(std::max<size_t>(2 * kCUs / std::max<size_t>(tiles(side), 1), 1), (size_t)std::max(p.stages / 4, 1));
-    p.stages_per_part = ((p.stages + p.parts - 1) / p.parts + 3) / 4 * 4;
-    p.parts = (p.stages + p.stages_per_part - 1) / p.stages_per_part;
-    p.ldp = ((size_t)Nout + 7) / 8 * 8;
-    p.codes = round256((size_t)M * p.blocks * 16);
-    p.scales = round256((size_t)M * p.blocks);
-    p.sums = p.parts > 1 ? round256((size_t)p.parts * M * p.ldp * 4) : 0;
-    return p;
-}
-
-template <typename T>
-static void mx4_launch_tiles(const Mx4Plan &p, Mx4Args a, hipStream_t st)
-{
-    a.tiles_m = p.tiles_m;
-    a.tiles_n = p.tiles_n;
-    a.stages = p.stages;
-    a.stages_per_part = p.stages_per_part;
-    a.parts = p.parts;
-    a.work = p.tiles_m * p.tiles_n * p.parts;
-    a.per_xcd = (a.work + kXCDs - 1) / kXCDs;
-    const dim3 grid((unsigned)a.per_xcd * kXCDs);
-    if (p.large) hipLaunchKernelGGL((mx4_product_kernel<4, 2, 2, 4, T>), grid, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((mx4_product_kernel<2, 2, 2, 2, T>), grid, dim3(256), 0, st, a);
+    Cut c = {};
+    const auto tiles = [&](int side) { return (long long)((I + side - 1) / side) * ((J + side - 1) / side); };
+    c.large = tiles(256) >= 192;
+    const int side = c.large ? 256 : 128;
+    Grid &g = c.grid;
+    g.tiles_i = (I + side - 1) / side;
+    g.tiles_j = (J + side - 1) / side;
+    g.stages = stages;
+    long long parts = 1;
+    if (!c.large) parts = std::min<long long>(std::max<long long>(2 * kCUs / std::max<long long>(tiles(side), 1), 1), std::max(stages / least, 1));
+    g.stages_per_part = (int)(((stages + parts - 1) / parts + step - 1) / step * step);
+    g.parts = (stages + g.stages_per_part - 1) / g.stages_per_part;
+    g.work = g.tiles_i * g.tiles_j * g.parts;
+    g.per_xcd = (g.work + kXCDs - 1) / kXCDs;
+    c.ldp = ((size_t)J + 7) / 8 * 8;
+    c.sums = g.parts > 1 ? round256((size_t)g.parts * I * c.ldp * 4) : 0;
+    return c;
 }
 
 // f(type tag) for the element type of t
@@ -413,16 +627,94 @@ static void with_type(lp_dtype t, F f)
     else f((_Float16 *)nullptr);
 }
 
-// y = act(sum of the parts + bias)
-static void join_parts(const float *sums, int parts, size_t part, size_t ldp, void *y, lp_dtype yt, size_t ldy, int I, int J, const float *bias, lp_actfn act,
-                       hipStream_t st)
+// out = act(sum of the parts + bias)
+static void join_parts(const float *sums, int parts, size_t part, size_t ldp, lp_dtype t, const Sink &out, int I, int J, hipStream_t st)
 {
     const unsigned per_row = (unsigned)(ldp / 8), total = per_row * (unsigned)I;
-    with_type(yt, [&](auto *tag) {
+    with_type(t, [&](auto *tag) {
         typedef std::remove_pointer_t<decltype(tag)> T;
-        hipLaunchKernelGGL(join_parts_kernel<T>, dim3((total + 255) / 256), dim3(256), 0, st, sums, parts, part, ldp, (T *)y, ldy, I, J, per_row,
-                           piece_magic(per_row), total, bias, act);
+        hipLaunchKernelGGL(join_parts_kernel<T>, dim3((total + 255) / 256), dim3(256), 0, st, sums, parts, part, ldp, out, J, per_row, piece_magic(per_row), total);
     });
+}
+
+struct Mx4Plan {
+    Cut cut;
+    size_t blocks;        // of 32 per row
+    size_t codes, scales; // workspace: quantized x (if the call brings floats), then the sums of the parts
+    size_t total() const { return codes + scales + cut.sums; }
+};
+
+static Mx4Plan mx4_plan(int M, int K, int Nout)
+{
+    Mx4Plan p = {};
+    p.blocks = mx4_blocks((size_t)K);
+    p.cut = cut_product(M, Nout, (int)(p.blocks / 8), 4, 4);
+    p.codes = round256((size_t)M * p.blocks * 16);
+    p.scales = round256((size_t)M * p.blocks);
+    return p;
+}
+
+template <typename T>
+static void mx4_launch(const Cut &c, const Mx4Args &a, hipStream_t st)
+{
+    const dim3 grid((unsigned)a.grid.per_xcd * kXCDs);
+    if (c.large) hipLaunchKernelGGL((mx4_product_kernel<4, 2, 2, 4, T>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((mx4_product_kernel<2, 2, 2, 2, T>), grid, dim3(256), 0, st, a);
+}
+
+// Gradients: workspace of the parts' sums, then of the bias's.
+struct GradPlan {
+    Cut cut;
+    size_t db;
+    size_t total() const { return cut.sums + db; }
+};
+
+static GradPlan grad_plan(int I, int J, int C, bool weights)
+{
+    GradPlan p = {};
+    p.cut = cut_product(I, J, std::max((C + 63) / 64, 1), 1, 8);
+    if (weights && p.cut.grid.parts > 1) p.db = round256((size_t)p.cut.grid.parts * (((size_t)I + 7) / 8 * 8) * 4);
+    return p;
+}
+
+template <bool WEIGHTS, typename T>
+static void grad_launch(const Cut &c, const GradArgs &a, hipStream_t st)
+{
+    const dim3 grid((unsigned)a.grid.per_xcd * kXCDs);
+    // Loads to LDS ask for words, and reach 2^31 bytes from a tile's first row.
+    const bool words = aligned_to(a.dy, 4) && a.ld % 2 == 0 && a.ld < ((size_t)1 << 22);
+    if (c.large) {
+        if (words) hipLaunchKernelGGL((gradient_kernel<4, 2, 2, 4, WEIGHTS, true, T>), grid, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((gradient_kernel<4, 2, 2, 4, WEIGHTS, false, T>), grid, dim3(512), 0, st, a);
+    } else {
+        if (words) hipLaunchKernelGGL((gradient_kernel<2, 2, 2, 2, WEIGHTS, true, T>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((gradient_kernel<2, 2, 2, 2, WEIGHTS, false, T>), grid, dim3(256), 0, st, a);
+    }
+}
+
+template <bool WEIGHTS>
+static void gradient(const GradPlan &p, GradArgs a, lp_dtype t, const Sink &out, float *dbias, unsigned char *work, hipStream_t st)
+{
+    a.grid = p.cut.grid;
+    a.db = dbias;
+    a.db_accumulate = out.accumulate;
+    if (p.cut.grid.parts > 1) {
+        float *sums = (float *)work, *db = (float *)(work + p.cut.sums);
+        const size_t part = (size_t)a.I * p.cut.ldp, db_part = ((size_t)a.I + 7) / 8 * 8;
+        a.out = Sink{sums, p.cut.ldp, part, nullptr, LP_ACT_NONE, 0};
+        if (dbias) {
+            a.db = db;
+            a.db_part = db_part;
+            a.db_accumulate = 0;
+        }
+        grad_launch<WEIGHTS, float>(p.cut, a, st);
+        join_parts(sums, a.grid.parts, part, p.cut.ldp, t, out, a.I, a.J, st);
+        if (dbias) join_parts(db, a.grid.parts, db_part, db_part, LP_F32, Sink{dbias, 0, 0, nullptr, LP_ACT_NONE, out.accumulate}, 1, a.I, st);
+    } else {
+        a.out = out;
+        if (t == LP_F32) grad_launch<WEIGHTS, float>(p.cut, a, st);
+        else grad_launch<WEIGHTS, __bf16>(p.cut, a, st);
+    }
 }
 
 } // namespace lp
@@ -430,6 +722,12 @@ static void join_parts(const float *sums, int parts, size_t part, size_t ldp, vo
 // ------------------------------------------------------------------------------------ C ABI
 
 using namespace lp;
+
+static lp_status workspace_status(size_t need, const void *workspace, size_t bytes)
+{
+    if (need && (!workspace || bytes < need)) return LP_EWORKSPACE;
+    return need && !aligned16(workspace) ? LP_EINVAL : LP_OK;
+}
 
 extern "C" lp_status lp_mx4_fc_workspace_bytes(int M, int K, int Nout, size_t *bytes_host)
 {
@@ -450,8 +748,7 @@ extern "C" lp_status lp_mx4_fc_fwd(int M, int K, int Nout, const void *x_dev, lp
     if (x_scales_dev ? !mx4_ok(x_dev, x_scales_dev) : !floats_ok(x_dev, xt, (size_t)K, ldx)) return LP_EINVAL;
     if (!mx4_ok(w_codes_dev, w_scales_dev) || !floats_ok(y_dev, yt, (size_t)Nout, ldy) || !aligned_to(bias_dev, 4)) return LP_EINVAL;
     const Mx4Plan p = mx4_plan(M, K, Nout);
-    if (p.total() && (!workspace_dev || workspace_bytes < p.total())) return LP_EWORKSPACE;
-    if (p.total() && !aligned16(workspace_dev)) return LP_EINVAL;
+    if (const lp_status s = workspace_status(p.total(), workspace_dev, workspace_bytes)) return s;
     hipStream_t st = as_stream(stream);
     clear_stale_error();
     unsigned char *work = (unsigned char *)workspace_dev;
@@ -463,20 +760,22 @@ extern "C" lp_status lp_mx4_fc_fwd(int M, int K, int Nout, const void *x_dev, lp
     a.M = M;
     a.N = Nout;
     a.blocks = (int)p.blocks;
+    a.grid = p.cut.grid;
     if (!a.xs) {
         mx4_quantize_launch(x_dev, xt, (size_t)M, (size_t)K, ldx, work, work + p.codes, st);
         a.xc = work;
         a.xs = work + p.codes;
     }
-    if (p.parts > 1) {
+    const Sink out{y_dev, ldy, 0, bias_dev, act, 0};
+    if (a.grid.parts > 1) {
         float *sums = (float *)(work + p.codes + p.scales);
-        const size_t part = (size_t)M * p.ldp;
-        a.out = Sink{sums, p.ldp, part, nullptr, LP_ACT_NONE};
-        mx4_launch_tiles<float>(p, a, st);
-        join_parts(sums, p.parts, part, p.ldp, y_dev, yt, ldy, M, Nout, bias_dev, act, st);
+        const size_t part = (size_t)M * p.cut.ldp;
+        a.out = Sink{sums, p.cut.ldp, part, nullptr, LP_ACT_NONE, 0};
+        mx4_launch<float>(p.cut, a, st);
+        join_parts(sums, a.grid.parts, part, p.cut.ldp, yt, out, M, Nout, st);
     } else {
-        a.out = Sink{y_dev, ldy, 0, bias_dev, act};
-        with_type(yt, [&](auto *tag) { mx4_launch_tiles<std::remove_pointer_t<decltype(tag)>>(p, a, st); });
+        a.out = out;
+        with_type(yt, [&](auto *tag) { mx4_launch<std::remove_pointer_t<decltype(tag)>>(p.cut, a, st); });
     }
     return launch_status();
 }
@@ -485,7 +784,7 @@ extern "C" lp_status lp_mx4_fc_dgrad_workspace_bytes(int M, int K, int Nout, siz
 {
     if (!bytes_host || !sizes_ok(M, K, Nout)) return LP_EINVAL;
     if (!sizes_taken(M, K, Nout)) return LP_EUNSUPPORTED;
-    *bytes_host = 0;
+    *bytes_host = M ? grad_plan(M, K, Nout, false).total() : 0;
     return LP_OK;
 }
 
@@ -497,11 +796,19 @@ extern "C" lp_status lp_mx4_fc_dgrad(int M, int K, int Nout, const void *dy_dev,
     if (!sizes_taken(M, K, Nout) || dxt == LP_F16) return LP_EUNSUPPORTED;
     if (M == 0) return LP_OK;
     if (!floats_ok(dy_dev, LP_BF16, (size_t)Nout, lddy) || !mx4_ok(w_codes_dev, w_scales_dev) || !floats_ok(dx_dev, dxt, (size_t)K, lddx)) return LP_EINVAL;
+    const GradPlan p = grad_plan(M, K, Nout, false);
+    if (const lp_status s = workspace_status(p.total(), workspace_dev, workspace_bytes)) return s;
     clear_stale_error();
-    const Bf16Rows a{(const __bf16 *)dy_dev, lddy};
-    const Mx4Rows b{(const unsigned char *)w_codes_dev, (const unsigned char *)w_scales_dev, mx4_blocks((size_t)K)};
-    hipLaunchKernelGGL((product_kernel<false, true, Bf16Rows, Mx4Rows>), product_grid(M, K), dim3(256), 0, as_stream(stream), a, b,
-                       Output{dx_dev, dxt, lddx, nullptr, LP_ACT_NONE, 0}, M, K, Nout);
+    GradArgs a = {};
+    a.dy = (const __bf16 *)dy_dev;
+    a.ld = lddy;
+    a.codes = (const unsigned char *)w_codes_dev;
+    a.scales = (const unsigned char *)w_scales_dev;
+    a.I = M;
+    a.J = K;
+    a.C = Nout;
+    a.blocks = (int)mx4_blocks((size_t)K);
+    gradient<false>(p, a, dxt, Sink{dx_dev, lddx, 0, nullptr, LP_ACT_NONE, 0}, nullptr, (unsigned char *)workspace_dev, as_stream(stream));
     return launch_status();
 }
 
@@ -509,7 +816,7 @@ extern "C" lp_status lp_ckpt8_fc_wgrad_workspace_bytes(int M, int K, int Nout, s
 {
     if (!bytes_host || !sizes_ok(M, K, Nout)) return LP_EINVAL;
     if (!sizes_taken(M, K, Nout)) return LP_EUNSUPPORTED;
-    *bytes_host = 0;
+    *bytes_host = grad_plan(Nout, K, M, true).total();
     return LP_OK;
 }
 
@@ -521,12 +828,18 @@ extern "C" lp_status lp_ckpt8_fc_wgrad(int M, int K, int Nout, const void *dy_de
     if (!sizes_taken(M, K, Nout) || dwt == LP_F16) return LP_EUNSUPPORTED;
     if (M && (!floats_ok(dy_dev, LP_BF16, (size_t)Nout, lddy) || !x_codes_dev || !aligned16(x_codes_dev) || !x_scales_dev)) return LP_EINVAL;
     if (!floats_ok(dw_dev, dwt, (size_t)K, lddw) || !aligned_to(dbias_dev, 4)) return LP_EINVAL;
-    hipStream_t st = as_stream(stream);
+    const GradPlan p = grad_plan(Nout, K, M, true);
+    if (const lp_status s = workspace_status(p.total(), workspace_dev, workspace_bytes)) return s;
     clear_stale_error();
-    const Bf16Rows a{(const __bf16 *)dy_dev, lddy};
-    const Ckpt8Rows b{(const signed char *)x_codes_dev, (const unsigned char *)x_scales_dev, ckpt8_blocks((size_t)K)};
-    hipLaunchKernelGGL((product_kernel<true, true, Bf16Rows, Ckpt8Rows>), product_grid(Nout, K), dim3(256), 0, st, a, b,
-                       Output{dw_dev, dwt, lddw, nullptr, LP_ACT_NONE, accumulate != 0}, Nout, K, M);
-    if (dbias_dev) hipLaunchKernelGGL(column_sums_kernel, dim3((Nout + 255) / 256), dim3(256), 0, st, a, M, Nout, dbias_dev, accumulate != 0);
+    GradArgs a = {};
+    a.dy = (const __bf16 *)dy_dev;
+    a.ld = lddy;
+    a.codes = (const unsigned char *)x_codes_dev;
+    a.scales = (const unsigned char *)x_scales_dev;
+    a.I = Nout;
+    a.J = K;
+    a.C = M;
+    a.blocks = (int)ckpt8_blocks((size_t)K);
+    gradient<true>(p, a, dwt, Sink{dw_dev, lddw, 0, nullptr, LP_ACT_NONE, accumulate != 0}, dbias_dev, (unsigned char *)workspace_dev, as_stream(stream));
     return launch_status();
 }

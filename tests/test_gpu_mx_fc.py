@@ -164,6 +164,49 @@ def test_weight_gradient(size):
     check_wgrad(*size, torch.float32, False, accumulate=True, extra=8)
 
 
+def test_gradients_take_the_whole_range_of_scales():
+    m, k, n = 150, 300, 140
+    g = torch.Generator().manual_seed(9)
+    dy = (torch.randn((m, n), generator=g) * 2.0 ** -20).bfloat16()
+    # ckpt8 blocks of every scale byte from 7 to 254, sums kept within 32 bits by the gradient's size
+    x = torch.randn((m, k), generator=g).double() * torch.exp2(torch.randint(-126, 125, (m, (k + 31) // 32), generator=g).double()).repeat_interleave(32, 1)[:, :k]
+    x = x.clamp(-3e38, 3e38).float()
+    codes, scales = mx.ckpt8_quantize(x.double().numpy())
+    assert scales.min() < 12 and scales.max() > 248
+    want, size = product(dy.cuda().t(), torch.from_numpy(mx.ckpt8_values(codes, scales, k)).cuda())
+    dw = torch.empty((n, k), device="cuda")
+    lp.lp_ckpt8_fc_wgrad(m, k, n, dy.cuda(), torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), dw,
+                         workspace=workspace(lp.lp_ckpt8_fc_wgrad_workspace_bytes(m, k, n)))
+    mx.close(dw, want, mx.product_error(size, m), torch.float32)
+    w = weights(n, k, 5, spread=120)
+    want, size = product(dy.cuda(), w[2])
+    dx = torch.empty((m, k), device="cuda")
+    lp.lp_mx4_fc_dgrad(m, k, n, dy.cuda(), w[0], w[1], dx, workspace=workspace(lp.lp_mx4_fc_dgrad_workspace_bytes(m, k, n)))
+    mx.close(dx, want, mx.product_error(size, n), torch.float32)
+
+
+@pytest.mark.parametrize("size", [(130, 200, 70), (70, 96, 130), (65, 300, 33)])
+def test_what_lies_behind_a_row_or_the_last_row_is_not_used(size):
+    """NaN between the rows of dY, and in the row after one that ends inside a tile."""
+    m, k, n = size
+    for extra in (1, 2, 8):
+        wide = torch.full((m, n + extra), float("nan"), dtype=torch.bfloat16, device="cuda")
+        dy = inputs(m, n, torch.bfloat16, 1).cuda()
+        wide[:, :n] = dy
+        bad = wide.clone()
+        bad[1] = float("nan")                                      # a whole row: row 1 of dX only
+        w, c = weights(n, k, 2), kept(m, k, 3)
+        outs = []
+        for d in (dy, wide[:, :n], bad[:, :n]):
+            dx, dw, db = torch.empty((m, k), device="cuda"), torch.empty((n, k), device="cuda"), torch.empty(n, device="cuda")
+            lp.lp_mx4_fc_dgrad(m, k, n, d, w[0], w[1], dx, workspace=workspace(lp.lp_mx4_fc_dgrad_workspace_bytes(m, k, n)))
+            lp.lp_ckpt8_fc_wgrad(m, k, n, d, c[0], c[1], dw, dbias=db, workspace=workspace(lp.lp_ckpt8_fc_wgrad_workspace_bytes(m, k, n)))
+            outs.append((dx, dw, db))
+        assert all(torch.equal(a, b) for a, b in zip(outs[0], outs[1]))
+        rows = torch.arange(m, device="cuda") != 1
+        assert torch.equal(outs[2][0][rows], outs[0][0][rows]) and bool(outs[2][0][1].isnan().all())
+
+
 def test_gradients_against_differences():
     """The product is linear in its input's values and in the weights' values: with 4-bit inputs that are exact, differences of the
     forward call give the gradients of sum(dY * Y)."""
