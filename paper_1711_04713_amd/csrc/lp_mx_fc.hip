@@ -28,7 +28,11 @@ __device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t from, unsigned 
 }
 
 // everything that this wave has asked for has arrived, and so it is in every other wave of the workgroup
-__device__ __forceinline__ void all_arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ void all_arrived()
+{
+    __builtin_amdgcn_s_waitcnt(0);
+    asm volatile("s_barrier" ::: "memory");
+}
 
 // -------------------------------------------------------------------------------- results
 
@@ -307,7 +311,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
 // instruction wants eight neighbouring positions of a row or column in a lane: those of dY's rows lie together in memory
 // (16-byte piece p of row r at place p ^ (r % 8), as above); tiles with the reduction along their rows are read by
 // ds_read_b64_tr_b16, which hands each of 16 lanes four rows' elements of its column.  Their rows are 512 (or 256) bytes, so
-// the four rows of such a read lie in the same banks unless the 64-byte pieces of row r change places with r % 4.
+// the four rows of such a read lie in the same banks unless the 64-byte pieces of row r change places with r % 4.  Decoded
+// codes also swap neighbouring 16 bytes where (column / 128 + row) is odd, for the sake of the writes.
 //
 // B is the row operand of the instruction, so that a lane ends up with four neighbouring columns of one row of D.
 struct GradArgs {
@@ -326,6 +331,14 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s *LdsV4;
+
+// Eight neighbouring positions of a lane's column: four rows from one place, four from the other.  (No load to LDS that is on
+// its way writes there: the arguments say so, or the compiler would wait for all of them first.)
+__device__ __forceinline__ v8s read_columns(const unsigned char *__restrict__ first, const unsigned char *__restrict__ next)
+{
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV4)first), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV4)next);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
 
 // n (at most 8) bfloat16 of a row as one 16-byte piece, zeros behind them
 __device__ __forceinline__ v4u load_piece(const __bf16 *p, int n)
@@ -349,32 +362,24 @@ template <bool WEIGHTS>
 struct RawBlock {
     v4u w[WEIGHTS ? 2 : 1];
     int e;
-    __device__ __forceinline__ void load(const GradArgs &a, int c, int block)
+    // what lies outside the descriptors comes as zeros
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t scales, unsigned block)
     {
-        if (c < a.C && block < a.blocks) {
-            const size_t at = (size_t)c * a.blocks + block;
-            const v4u *from = reinterpret_cast<const v4u *>(a.codes) + at * (WEIGHTS ? 2 : 1);
 #pragma unroll
-            for (int k = 0; k < (WEIGHTS ? 2 : 1); ++k) w[k] = from[k];
-            e = a.scales[at];
-        } else {
-#pragma unroll
-            for (int k = 0; k < (WEIGHTS ? 2 : 1); ++k) w[k] = 0;
-            e = 127;
-        }
+        for (int k = 0; k < (WEIGHTS ? 2 : 1); ++k)
+            w[k] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(codes, block * (WEIGHTS ? 32 : 16) + 16 * k, 0, 0));
+        e = __builtin_amdgcn_raw_buffer_load_b8(scales, block, 0, 0);
     }
     // sixteen-byte piece k of the block's values: elements 8 k .. 8 k + 7
     __device__ __forceinline__ v4u piece(int k) const
     {
         if constexpr (WEIGHTS) {
-            // q + 128 in the low byte of 2^23 is the number 2^23 + 128 + q
             const float s = power_of_byte(e - 6);
             v4u r;
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                const unsigned word = w[k >> 1][(k & 1) * 2 + (d >> 1)] ^ 0x80808080u;
-                const float lo = (__uint_as_float(__builtin_amdgcn_perm(0x4B000000u, word, 0x07060500u | (2 * (d & 1)))) - 8388736.0f) * s;
-                const float hi = (__uint_as_float(__builtin_amdgcn_perm(0x4B000000u, word, 0x07060501u | (2 * (d & 1)))) - 8388736.0f) * s;
+                const unsigned word = w[k >> 1][(k & 1) * 2 + (d >> 1)] >> (16 * (d & 1));
+                const float lo = (float)(signed char)word * s, hi = (float)(signed char)(word >> 8) * s;
                 r[d] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); // (their low halves are zero)
             }
             return r;
@@ -451,14 +456,25 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
         }
     };
 
-    // B: thread's row of the stage and block of the row
+    // B: thread's row of the stage and block of the row.  The descriptors start at a stage's first row and end with the tensor.
     RawBlock<WEIGHTS> raw;
     const int brow = threadIdx.x / (TJ / 32), bblock = threadIdx.x % (TJ / 32);
+    const unsigned bat = j0 / 32 + bblock < a.blocks ? (unsigned)brow * (unsigned)a.blocks + (unsigned)(j0 / 32 + bblock) : 0x07ffffffu;
+    // (eight lanes that write together hold one piece of each 64 bytes of a row, or of two rows: half of them swap neighbours)
     unsigned char *const bplace = lds + ABYTES + brow * BROW + (bblock ^ (brow & 3)) * 64;
-    auto load_b = [&](int t) __attribute__((always_inline)) { raw.load(a, t < last ? t * 64 + brow : a.C, j0 / 32 + bblock); };
+    const int bswap = ((bblock >> 2 ^ brow) & 1) * 16;
+    const int end = min(last * 64, a.C);
+    auto load_b = [&](int t) __attribute__((always_inline)) {
+        constexpr int BLOCK = WEIGHTS ? 32 : 16;
+        const long long left = std::min(std::max((long long)(end - t * 64) * a.blocks, 0LL), 0x07ffffffLL); // blocks
+        const int scales = __builtin_amdgcn_readfirstlane((int)left), codes = scales * BLOCK;
+        const size_t from = (size_t)t * 64 * a.blocks;
+        raw.load(__builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.codes) + from * BLOCK, 0, codes, 0x00020000),
+                 __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.scales) + from, 0, scales, 0x00020000), bat);
+    };
     auto place_b = [&](int buf, int from, int to) __attribute__((always_inline)) {
 #pragma unroll
-        for (int k = from; k < to; ++k) *(v4u *)(bplace + buf * STAGE + k * 16) = raw.piece(k);
+        for (int k = from; k < to; ++k) *(v4u *)(bplace + buf * STAGE + (k * 16 ^ bswap)) = raw.piece(k);
     };
 
     v16f acc[NB][MB] = {};
@@ -470,11 +486,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
 #pragma unroll
     for (int b = 0; b < MB; ++b) apos[b] = WEIGHTS ? tr_place((wm * MB + b) * 32, AROW) : ((wm * MB + b) * 32 + l32) * 128;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) bpos[b] = ABYTES + tr_place((wn * NB + b) * 32, BROW);
-    auto tr_read = [&](int pos, int row_bytes) __attribute__((always_inline)) {
-        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV4)(lds + pos)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV4)(lds + pos + 4 * row_bytes));
-        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
+    for (int b = 0; b < NB; ++b) bpos[b] = ABYTES + (tr_place((wn * NB + b) * 32, BROW) ^ (((wn * NB + b) >> 2 ^ tr_row) & 1) * 16);
+    auto tr_read = [&](int pos, int row_bytes) __attribute__((always_inline)) { return read_columns(lds + pos, lds + pos + 4 * row_bytes); };
     auto fragments = [&](int buf, int s) __attribute__((always_inline)) {
 #pragma unroll
         for (int b = 0; b < MB; ++b) {
