@@ -338,57 +338,86 @@ def lp_maxpool2x2(x_codes, y_codes, N, H, W, C, n_bits):
 _dtypes = {}
 
 
+def _first_device():
+    import torch
+
+    global _device
+    _dtypes.update({torch.float32: LP_F32, torch.bfloat16: LP_BF16, torch.float16: LP_F16})
+    if not torch.cuda.is_available():
+        return None                            # no tensor is there
+    device = torch.cuda.current_device()      # initialises the GPU
+    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return device
+
+
+_device = _first_device
+
+
 def _dtype(t):
     """lp_dtype of a tensor; -1, which every call refuses, where there is none."""
-    if not _dtypes:
-        import torch
-
-        _dtypes.update({torch.float32: LP_F32, torch.bfloat16: LP_BF16, torch.float16: LP_F16})
     return _dtypes.get(t.dtype, -1)
 
 
-def _need(ok, what, why):
-    """Raises what the C entry point cannot see for itself: the tensors' own sizes and types."""
-    if not ok:
-        raise ValueError("%s: %s" % (what, why))
+def _refuse(what, why):
+    raise ValueError("%s: %s" % (what, why))
 
 
-def _here(t, what, name):
-    """Raises for a tensor that is not on the current GPU, whose stream the call goes to."""
-    if t is not None:
-        at = t.get_device()
-        _need(at >= 0 and at == _device(), what, "%s is not on the current GPU" % name)
+# What the C entry points cannot see for themselves: where the tensors are, their own sizes and strides.
+
+def _here(t, device, what, name):
+    """Address of a tensor that has to be on the current GPU, whose stream the call goes to (None: a null pointer)."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        _refuse(what, "%s is not on the current GPU" % name)
+    return t.data_ptr()
 
 
-def _device():
-    import torch
-
-    return torch.cuda.current_device()
-
-
-def _rows(t, rows, cols, what, name):
-    """Row stride of a float tensor [rows][cols]."""
-    _need(t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols and (cols <= 1 or t.stride(1) == 1), what,
-          "%s is not a [%d][%d] tensor with unit column stride" % (name, rows, cols))
-    _here(t, what, name)
-    return t.stride(0) if rows > 1 else max(cols, 1)
+def _rows(t, rows, cols, device, what, name):
+    """Address and row stride of a float tensor [rows][cols]."""
+    if t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
+        _refuse(what, "%s is not a [%d][%d] tensor with unit column stride" % (name, rows, cols))
+    if t.get_device() != device:
+        _refuse(what, "%s is not on the current GPU" % name)
+    return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, 1)
 
 
-def _held(codes, scales, rows, blocks, block_bytes, what, name):
-    """codes and scales of a microscaled tensor are whole and dense."""
-    _need(codes.numel() * codes.element_size() == rows * blocks * block_bytes and codes.is_contiguous() and
-          scales.numel() * scales.element_size() == rows * blocks and scales.is_contiguous(), what,
-          "%s: codes or scales are not those of %d rows of %d blocks" % (name, rows, blocks))
-    _here(codes, what, name)
-    _here(scales, what, name)
+def _dense(t, nbytes, device, what, name):
+    """Address of nbytes of dense memory."""
+    if t.nbytes != nbytes or not t.is_contiguous():
+        _refuse(what, "%s does not hold %d dense bytes" % (name, nbytes))
+    if t.get_device() != device:
+        _refuse(what, "%s is not on the current GPU" % name)
+    return t.data_ptr()
 
 
-def _mx4(codes, scales, rows, cols, what, name):
-    _held(codes, scales, rows, (cols + 255) // 256 * 8, 16, what, name)
+def _mx4(codes, scales, rows, cols, device, what, name):
+    blocks = rows * ((cols + 255) // 256 * 8)
+    return _dense(codes, 16 * blocks, device, what, name + "'s codes"), _dense(scales, blocks, device, what, name + "'s scales")
 
 
-def _ckpt8(codes, scales, rows, cols, what, name):
-    _held(codes, scales, rows, (cols + 31) // 32, 32, what, name)
+def _ckpt8(codes, scales, rows, cols, device, what, name):
+    blocks = rows * ((cols + 31) // 32)
+    return _dense(codes, 32 * blocks, device, what, name + "'s codes"), _dense(scales, blocks, device, what, name + "'s scales")
+
+
+def _vector(t, n, device, what, name):
+    """Address of n dense float32 (None: a null pointer)."""
+    if t is None:
+        return None
+    if _dtype(t) != LP_F32:
+        _refuse(what, "%s is not float32" % name)
+    return _dense(t, 4 * n, device, what, name)
+
+
+def _workspace(t, device, what):
+    """Address and bytes of a workspace."""
+    return (None, 0) if t is None else (_here(t, device, what, "workspace"), t.nbytes)
+
+
+def _bf16(t, what, name):
+    if _dtype(t) != LP_BF16:
+        _refuse(what, "%s is not bfloat16" % name)
 
 
 def _two_sizes(what, rows, cols):
@@ -403,14 +432,6 @@ def _fc_workspace_bytes(what, M, K, Nout):
     return n.value
 
 
-def _workspace(t, what):
-    """Address and bytes of a workspace."""
-    if t is None:
-        return None, 0
-    _here(t, what, "workspace")
-    return t.data_ptr(), t.numel() * t.element_size()
-
-
 def lp_mx4_bytes(rows, cols):
     """(codes, scales) bytes of an mx4 tensor."""
     return _two_sizes("lp_mx4_bytes", rows, cols)
@@ -423,20 +444,20 @@ def lp_ckpt8_bytes(rows, cols):
 
 def lp_mx4_quantize(x, codes, scales, r=LP_ROUND_NEAREST_EVEN, seed=0, zero_count=None, sat_count=None):
     """x: [rows][cols] float32, bfloat16 or float16."""
+    what, device = "lp_mx4_quantize", _device()
     rows, cols = x.shape
-    ld = _rows(x, rows, cols, "lp_mx4_quantize", "x")
-    _mx4(codes, scales, rows, cols, "lp_mx4_quantize", "x")
-    _here(zero_count, "lp_mx4_quantize", "zero_count")
-    _here(sat_count, "lp_mx4_quantize", "sat_count")
-    _check(load().lp_mx4_quantize(_ptr(x), _dtype(x), rows, cols, ld, _ptr(codes), _ptr(scales), r, seed, _ptr(zero_count),
-                                  _ptr(sat_count), _stream()), "lp_mx4_quantize")
+    px, ldx = _rows(x, rows, cols, device, what, "x")
+    pc, ps = _mx4(codes, scales, rows, cols, device, what, "x")
+    _check(load().lp_mx4_quantize(px, _dtype(x), rows, cols, ldx, pc, ps, r, seed, _here(zero_count, device, what, "zero_count"),
+                                  _here(sat_count, device, what, "sat_count"), _stream()), what)
 
 
 def lp_mx4_dequantize(codes, scales, y):
+    what, device = "lp_mx4_dequantize", _device()
     rows, cols = y.shape
-    ld = _rows(y, rows, cols, "lp_mx4_dequantize", "y")
-    _mx4(codes, scales, rows, cols, "lp_mx4_dequantize", "y")
-    _check(load().lp_mx4_dequantize(_ptr(codes), _ptr(scales), rows, cols, _ptr(y), _dtype(y), ld, _stream()), "lp_mx4_dequantize")
+    py, ldy = _rows(y, rows, cols, device, what, "y")
+    pc, ps = _mx4(codes, scales, rows, cols, device, what, "y")
+    _check(load().lp_mx4_dequantize(pc, ps, rows, cols, py, _dtype(y), ldy, _stream()), what)
 
 
 def lp_mx4_fc_workspace_bytes(M, K, Nout):
@@ -445,26 +466,16 @@ def lp_mx4_fc_workspace_bytes(M, K, Nout):
 
 def lp_mx4_fc_fwd(M, K, Nout, x, w_codes, w_scales, y, x_scales=None, bias=None, act=LP_ACT_NONE, workspace=None):
     """x: floats [M][K], or the codes of an mx4 tensor whose scales are x_scales.  bias: float32 [Nout]."""
+    what, device = "lp_mx4_fc_fwd", _device()
     if x_scales is None:
-        xt, ldx = _dtype(x), _rows(x, M, K, "lp_mx4_fc_fwd", "x")
+        (px, ldx), pxs, xt = _rows(x, M, K, device, what, "x"), None, _dtype(x)
     else:
-        xt, ldx = LP_F32, 0
-        _mx4(x, x_scales, M, K, "lp_mx4_fc_fwd", "x")
-    ldy = _rows(y, M, Nout, "lp_mx4_fc_fwd", "y")
-    _mx4(w_codes, w_scales, Nout, K, "lp_mx4_fc_fwd", "w")
-    _vector(bias, Nout, "lp_mx4_fc_fwd", "bias")
-    _check(load().lp_mx4_fc_fwd(M, K, Nout, _ptr(x), xt, ldx, _ptr(x_scales), _ptr(w_codes), _ptr(w_scales), _ptr(bias), _ptr(y),
-                                _dtype(y), ldy, act, *_workspace(workspace, "lp_mx4_fc_fwd"), _stream()), "lp_mx4_fc_fwd")
-
-
-def _vector(t, n, what, name):
-    if t is not None:
-        _need(_dtype(t) == LP_F32 and t.numel() == n and t.is_contiguous(), what, "%s is not %d dense float32" % (name, n))
-        _here(t, what, name)
-
-
-def _bf16(t, what, name):
-    _need(_dtype(t) == LP_BF16, what, "%s is not bfloat16" % name)
+        (px, pxs), ldx, xt = _mx4(x, x_scales, M, K, device, what, "x"), 0, LP_F32
+    py, ldy = _rows(y, M, Nout, device, what, "y")
+    pc, ps = _mx4(w_codes, w_scales, Nout, K, device, what, "w")
+    pb = _vector(bias, Nout, device, what, "bias")
+    pw, nw = _workspace(workspace, device, what)
+    _check(load().lp_mx4_fc_fwd(M, K, Nout, px, xt, ldx, pxs, pc, ps, pb, py, _dtype(y), ldy, act, pw, nw, _stream()), what)
 
 
 def lp_mx4_fc_dgrad_workspace_bytes(M, K, Nout):
@@ -473,40 +484,47 @@ def lp_mx4_fc_dgrad_workspace_bytes(M, K, Nout):
 
 def lp_mx4_fc_dgrad(M, K, Nout, dy, w_codes, w_scales, dx, workspace=None):
     """dy: bfloat16 [M][Nout]; dx: bfloat16 or float32 [M][K]."""
-    _bf16(dy, "lp_mx4_fc_dgrad", "dy")
-    lddy, lddx = _rows(dy, M, Nout, "lp_mx4_fc_dgrad", "dy"), _rows(dx, M, K, "lp_mx4_fc_dgrad", "dx")
-    _mx4(w_codes, w_scales, Nout, K, "lp_mx4_fc_dgrad", "w")
-    _check(load().lp_mx4_fc_dgrad(M, K, Nout, _ptr(dy), lddy, _ptr(w_codes), _ptr(w_scales), _ptr(dx), _dtype(dx), lddx, *_workspace(workspace, "lp_mx4_fc_dgrad"), _stream()), "lp_mx4_fc_dgrad")
+    what, device = "lp_mx4_fc_dgrad", _device()
+    _bf16(dy, what, "dy")
+    pdy, lddy = _rows(dy, M, Nout, device, what, "dy")
+    pdx, lddx = _rows(dx, M, K, device, what, "dx")
+    pc, ps = _mx4(w_codes, w_scales, Nout, K, device, what, "w")
+    pw, nw = _workspace(workspace, device, what)
+    _check(load().lp_mx4_fc_dgrad(M, K, Nout, pdy, lddy, pc, ps, pdx, _dtype(dx), lddx, pw, nw, _stream()), what)
 
 
 def lp_ckpt8_save(x, codes, scales, act=LP_ACT_NONE, y=None, r=LP_ROUND_NEAREST_EVEN, seed=0):
-    """Keeps x in codes and scales; y (nullable, of x's type) receives act(x)."""
+    """Keeps x in codes and scales; y (nullable, of x's type; may be x) receives act(x)."""
+    what, device = "lp_ckpt8_save", _device()
     rows, cols = x.shape
-    ldx = _rows(x, rows, cols, "lp_ckpt8_save", "x")
-    ldy = 0
+    px, ldx = _rows(x, rows, cols, device, what, "x")
+    py, ldy = None, 0
     if y is not None:
-        _need(y.dtype == x.dtype, "lp_ckpt8_save", "y is not of x's type")
-        ldy = _rows(y, rows, cols, "lp_ckpt8_save", "y")
-    _ckpt8(codes, scales, rows, cols, "lp_ckpt8_save", "x")
-    _check(load().lp_ckpt8_save(_ptr(x), _dtype(x), rows, cols, ldx, _ptr(codes), _ptr(scales), r, seed, act, _ptr(y), ldy,
-                                _stream()), "lp_ckpt8_save")
+        if y.dtype != x.dtype:
+            _refuse(what, "y is not of x's type")
+        py, ldy = _rows(y, rows, cols, device, what, "y")
+    pc, ps = _ckpt8(codes, scales, rows, cols, device, what, "x")
+    _check(load().lp_ckpt8_save(px, _dtype(x), rows, cols, ldx, pc, ps, r, seed, act, py, ldy, _stream()), what)
 
 
 def lp_ckpt8_load(codes, scales, y):
+    what, device = "lp_ckpt8_load", _device()
     rows, cols = y.shape
-    ldy = _rows(y, rows, cols, "lp_ckpt8_load", "y")
-    _ckpt8(codes, scales, rows, cols, "lp_ckpt8_load", "y")
-    _check(load().lp_ckpt8_load(_ptr(codes), _ptr(scales), rows, cols, _ptr(y), _dtype(y), ldy, _stream()), "lp_ckpt8_load")
+    py, ldy = _rows(y, rows, cols, device, what, "y")
+    pc, ps = _ckpt8(codes, scales, rows, cols, device, what, "y")
+    _check(load().lp_ckpt8_load(pc, ps, rows, cols, py, _dtype(y), ldy, _stream()), what)
 
 
 def lp_ckpt8_act_bwd(codes, scales, dy, dx, act):
     """dx = dy * act'(kept value); dx may be dy."""
+    what, device = "lp_ckpt8_act_bwd", _device()
     rows, cols = dy.shape
-    _need(dx.dtype == dy.dtype, "lp_ckpt8_act_bwd", "dx is not of dy's type")
-    lddy, lddx = _rows(dy, rows, cols, "lp_ckpt8_act_bwd", "dy"), _rows(dx, rows, cols, "lp_ckpt8_act_bwd", "dx")
-    _ckpt8(codes, scales, rows, cols, "lp_ckpt8_act_bwd", "dy")
-    _check(load().lp_ckpt8_act_bwd(_ptr(codes), _ptr(scales), rows, cols, _ptr(dy), _dtype(dy), lddy, act, _ptr(dx), lddx,
-                                   _stream()), "lp_ckpt8_act_bwd")
+    if dx.dtype != dy.dtype:
+        _refuse(what, "dx is not of dy's type")
+    pdy, lddy = _rows(dy, rows, cols, device, what, "dy")
+    pdx, lddx = _rows(dx, rows, cols, device, what, "dx")
+    pc, ps = _ckpt8(codes, scales, rows, cols, device, what, "dy")
+    _check(load().lp_ckpt8_act_bwd(pc, ps, rows, cols, pdy, _dtype(dy), lddy, act, pdx, lddx, _stream()), what)
 
 
 def lp_ckpt8_fc_wgrad_workspace_bytes(M, K, Nout):
@@ -515,9 +533,11 @@ def lp_ckpt8_fc_wgrad_workspace_bytes(M, K, Nout):
 
 def lp_ckpt8_fc_wgrad(M, K, Nout, dy, x_codes, x_scales, dw, dbias=None, accumulate=False, workspace=None):
     """dy: bfloat16 [M][Nout]; dw: bfloat16 or float32 [Nout][K]; dbias: float32 [Nout]."""
-    _bf16(dy, "lp_ckpt8_fc_wgrad", "dy")
-    lddy, lddw = _rows(dy, M, Nout, "lp_ckpt8_fc_wgrad", "dy"), _rows(dw, Nout, K, "lp_ckpt8_fc_wgrad", "dw")
-    _ckpt8(x_codes, x_scales, M, K, "lp_ckpt8_fc_wgrad", "x")
-    _vector(dbias, Nout, "lp_ckpt8_fc_wgrad", "dbias")
-    _check(load().lp_ckpt8_fc_wgrad(M, K, Nout, _ptr(dy), lddy, _ptr(x_codes), _ptr(x_scales), _ptr(dw), _dtype(dw), lddw, _ptr(dbias),
-                                    int(bool(accumulate)), *_workspace(workspace, "lp_ckpt8_fc_wgrad"), _stream()), "lp_ckpt8_fc_wgrad")
+    what, device = "lp_ckpt8_fc_wgrad", _device()
+    _bf16(dy, what, "dy")
+    pdy, lddy = _rows(dy, M, Nout, device, what, "dy")
+    pdw, lddw = _rows(dw, Nout, K, device, what, "dw")
+    pc, ps = _ckpt8(x_codes, x_scales, M, K, device, what, "x")
+    pb = _vector(dbias, Nout, device, what, "dbias")
+    pw, nw = _workspace(workspace, device, what)
+    _check(load().lp_ckpt8_fc_wgrad(M, K, Nout, pdy, lddy, pc, ps, pdw, _dtype(dw), lddw, pb, int(bool(accumulate)), pw, nw, _stream()), what)

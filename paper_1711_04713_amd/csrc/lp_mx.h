@@ -64,7 +64,30 @@ __device__ __forceinline__ void store8(T *p, int n, v8f v)
     }
 }
 
-// ---------------------------------------------------------------------------------- decoders
+// ------------------------------------------------------------- blocks of 32 in four neighbouring lanes
+
+// largest of the four lanes that hold a block
+__device__ __forceinline__ int block_max(int v)
+{
+    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true)); // lanes 1 0 3 2
+    return max(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true)); // lanes 2 3 0 1
+}
+
+// biased exponent of the block's largest finite magnitude
+__device__ __forceinline__ int block_exponent(const v8f &v)
+{
+    int m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int b = (int)(__float_as_uint(v[j]) & 0x7fffffffu);
+        m = max(m, b < 0x7f800000 ? b : 0);
+    }
+    return block_max(m) >> 23;
+}
+
+__device__ __forceinline__ int mx4_scale_byte(int exponent) { return min(max(exponent - 2, 2), 252); }
+
+// ---------------------------------------------------------------------------- codes and values
 
 __device__ __forceinline__ float power_of_byte(int e) { return __uint_as_float((unsigned)e << 23); } // 2^(e - 127), 1 <= e <= 254
 
@@ -75,6 +98,19 @@ __device__ __forceinline__ v8f mx4_values(unsigned w, int e)
     const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
     const v2f c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
     return v8f{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+
+// eight floats to one word of mx4 codes, nearest even, by the hardware's conversion (which divides by 2^(e - 127) and
+// saturates); NaN becomes 0
+__device__ __forceinline__ unsigned mx4_word(v8f v, int e)
+{
+    const float s = power_of_byte(e);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = v[j] == v[j] ? v[j] : 0.0f;
+    unsigned w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], s, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], s, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], s, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], s, 3);
 }
 
 // eight ckpt8 elements (two words of codes) times 2^(e - 133)

@@ -28,25 +28,6 @@ static bool piece_grid(size_t rows, size_t cols, size_t blocks, PieceGrid *g)
 
 static dim3 blocks_for(const PieceGrid &g) { return dim3((g.total + kThreads - 1) / kThreads); }
 
-// largest of the four lanes that hold a block
-__device__ __forceinline__ int block_max(int v)
-{
-    v = max(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true)); // lanes 1 0 3 2
-    return max(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true)); // lanes 2 3 0 1
-}
-
-// biased exponent of the block's largest finite magnitude
-__device__ __forceinline__ int block_exponent(const v8f &v)
-{
-    int m = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int b = (int)(__float_as_uint(v[j]) & 0x7fffffffu);
-        m = max(m, b < 0x7f800000 ? b : 0);
-    }
-    return block_max(m) >> 23;
-}
-
 // the draws of elements i .. i + 7
 __device__ __forceinline__ void draws8(uint64_t i, uint64_t seed, uint32_t (&w)[8])
 {
@@ -62,7 +43,7 @@ __device__ __forceinline__ void draws8(uint64_t i, uint64_t seed, uint32_t (&w)[
 
 // One magnitude t >= 0 (in units of the block's scale, exact) to its code 0..8; 8 does not exist and saturates.  The
 // magnitudes go in steps of 1/2 below 2, of 1 below 4 and of 2 above: with t in units of the step, the codes of a segment are
-// consecutive, and an even code is an even whole number there.
+// consecutive.  (Nearest even is the hardware's own conversion, mx4_word.)
 template <int MODE>
 __device__ __forceinline__ int mx4_code(float t, uint32_t draw)
 {
@@ -72,8 +53,6 @@ __device__ __forceinline__ int mx4_code(float t, uint32_t draw)
     float r;
     if (MODE == LP_ROUND_NEAREST_AWAY) {
         r = roundf(u);
-    } else if (MODE == LP_ROUND_NEAREST_EVEN) {
-        r = rintf(u);
     } else {
         r = floorf(u);
         r += (double)draw < (double)(u - r) * 4294967296.0 ? 1.0f : 0.0f;
@@ -93,19 +72,31 @@ __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(const T *__restr
         const unsigned col = 8 * piece;
         const int n = (int)min(g.cols - min(col, g.cols), 8u);
         v8f v = load8(x + row * ldx + col, n);
-        const int e = min(max(block_exponent(v) - 2, 2), 252);
-        const float inv = power_of_byte(254 - e);
-        uint32_t draw[8] = {};
-        if constexpr (MODE == LP_ROUND_STOCHASTIC) draws8((uint64_t)row * g.cols + col, seed, draw);
+        const int e = mx4_scale_byte(block_exponent(v));
         unsigned w = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float a = v[j] == v[j] ? v[j] : 0.0f;
-            const int c = mx4_code<MODE>(fabsf(a) * inv, draw[j]);
-            w |= (unsigned)(min(c, 7) | (a < 0.0f ? 8 : 0)) << (4 * j);
+        if constexpr (MODE == LP_ROUND_NEAREST_EVEN) {
+            w = mx4_word(v, e);
             if (COUNT) {
-                zeros += j < n && c == 0;
-                sats += j < n && c > 7;
+                const float over = 7.0f * power_of_byte(e); // rounds to 8
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    zeros += j < n && (w >> (4 * j) & 7) == 0;
+                    sats += j < n && fabsf(v[j]) >= over;
+                }
+            }
+        } else {
+            const float inv = power_of_byte(254 - e);
+            uint32_t draw[8] = {};
+            if constexpr (MODE == LP_ROUND_STOCHASTIC) draws8((uint64_t)row * g.cols + col, seed, draw);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float a = v[j] == v[j] ? v[j] : 0.0f;
+                const int c = mx4_code<MODE>(fabsf(a) * inv, draw[j]);
+                w |= (unsigned)(min(c, 7) | (a < 0.0f ? 8 : 0)) << (4 * j);
+                if (COUNT) {
+                    zeros += j < n && c == 0;
+                    sats += j < n && c > 7;
+                }
             }
         }
         codes[p] = w;

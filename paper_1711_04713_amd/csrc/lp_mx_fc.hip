@@ -27,12 +27,16 @@ __device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t from, unsigned 
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (LdsPtr)to, 4, lane_offset, offset, 0, 0);
 }
 
-// everything that this wave has asked for has arrived, and so it is in every other wave of the workgroup
-__device__ __forceinline__ void all_arrived()
+// Everything that this wave has asked for has arrived but the last LATER loads from memory, and so it is in every other wave of
+// the workgroup.
+template <int LATER>
+__device__ __forceinline__ void arrived_but()
 {
-    __builtin_amdgcn_s_waitcnt(0);
+    static_assert(LATER < 64, "what the counter holds");
+    __builtin_amdgcn_s_waitcnt((LATER & 15) | (LATER >> 4) << 14 | 7 << 4);
     asm volatile("s_barrier" ::: "memory");
 }
+__device__ __forceinline__ void all_arrived() { arrived_but<0>(); }
 
 // -------------------------------------------------------------------------------- results
 
@@ -139,7 +143,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float *__restrict
 // A workgroup owns TM rows of x times TN rows of w, one wave MB x NB blocks of 32 x 32; two waves per SIMD, so that the
 // one's reads and address arithmetic hide behind the other's products.  A stage is 256 positions: 128 bytes of each row (a
 // whole cache line: 64 bytes of twice as many rows come at 54 GB/s a CU instead of 90), brought to LDS by loads that do not
-// pass through registers, into one of two buffers; one stage is on its way while the other is multiplied.  16-byte piece p
+// pass through registers, into one of BUFFERS buffers; the others are on their way while one is multiplied.  16-byte piece p
 // of row r lies at place p ^ (r % 8) of the row, so that the eight rows that a read takes together lie in different banks.
 // Within a stage the order of the reduction is free as long as both sides share it: in step s (of four) the lower half of
 // the lanes takes block s, the upper half block 4 + s, so that a lane's scale bytes of a stage are one word.  Scale bytes
@@ -148,19 +152,20 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float *__restrict
 // Weights are the row operand: a lane ends up with four neighbouring columns of one row of y.
 struct Mx4Args {
     const unsigned char *xc, *xs, *wc, *ws;
-    int M, N, blocks;
+    int M, N, K, blocks;
     Grid grid; // stages_per_part: a multiple of 4
     Sink out;
 };
 
-template <int MB, int NB, int WM, int WN, typename OutT>
+template <int MB, int NB, int WM, int WN, int BUFFERS, typename OutT>
 __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Args a)
 {
+    static_assert(BUFFERS == 2 || BUFFERS == 4, "a stage's buffer is known where it is written out");
     constexpr int TM = MB * 32 * WM, TN = NB * 32 * WN, WAVES = WM * WN, ROWS = TM + TN, STAGE = ROWS * 128, PER = ROWS / 8 / WAVES;
     constexpr int SROWS = ROWS / WAVES, SPER = SROWS / 32; // rows whose scale bytes a wave brings, loads that takes
     static_assert(TM % SROWS == 0, "of one tensor");
     // (the scale bytes of a row's stages that do not exist are read too, from whatever follows: 32 bytes more)
-    __shared__ __align__(1024) unsigned char lds[2 * STAGE + ROWS * 32 + 32];
+    __shared__ __align__(1024) unsigned char lds[BUFFERS * STAGE + ROWS * 32 + 32];
     static_assert(WAVES * result_bytes(NB) <= (int)sizeof(lds), "results pass through the same memory");
     Place p;
     if (!find_place(a.grid, &p)) return;
@@ -196,7 +201,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
     constexpr std::integral_constant<int, PER> L3;
     // Scale bytes of stages t .. t + 3 (t a multiple of 4), 32 for each row, two lanes a row; where a row ends before that its last
     // 32.  Rows of fewer than 32 come a word a lane: the rows' eight bytes of the first stage, then those of the next.
-    unsigned char *const scales = lds + 2 * STAGE;
+    unsigned char *const scales = lds + BUFFERS * STAGE;
     const bool narrow = a.blocks < 32;
     const int row_step = narrow ? 8 : 32, stage_step = narrow ? ROWS * 8 : 8;
     auto scales_of = [&](int size) __attribute__((always_inline)) {
@@ -257,31 +262,34 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
     }                                                                                                                                       \
     __builtin_amdgcn_sched_barrier(0);
     // Stage t, number Q of its four.  At its last step the next stage has arrived in every wave, its own buffer is free and the
-    // stage after that is asked for, over three steps: 64 loads at once take the address unit so long that every wave waits
-    // for its turn.  At the first one's the scale bytes are in registers and the next four's are asked for.
+    // stage that will have it is asked for, over three steps: 64 loads at once take the address unit so long that every wave
+    // waits for its turn.  At the first one's the scale bytes are in registers and the next four's are asked for.
     auto whole_stage = [&](int t, auto number) __attribute__((always_inline)) {
-        constexpr int Q = decltype(number)::value, B = Q & 1;
+        constexpr int Q = decltype(number)::value, B = Q % BUFFERS, BEFORE = (Q + BUFFERS - 1) % BUFFERS;
+        // loads that may still be on their way when the next stage has arrived: the stages behind it, the scale bytes
+        constexpr int LATER = (BUFFERS - 2) * PER + (Q >= 1 && Q <= BUFFERS - 2 ? SPER : 0);
         __builtin_amdgcn_sched_barrier(0);
         fragments(B, 1);
-        stage(t + 1, B ^ 1, L1, L2);
+        stage(t + BUFFERS - 1, BEFORE, L1, L2);
         LP_STEP(Q, 0, true)
         fragments(B, 2);
-        stage(t + 1, B ^ 1, L2, L3);
+        stage(t + BUFFERS - 1, BEFORE, L2, L3);
         LP_STEP(Q, 1, true)
         fragments(B, 3);
         LP_STEP(Q, 2, false)
-        all_arrived();
-        fragments(B ^ 1, 0);
-        stage(t + 2, B, L0, L1);
+        arrived_but<LATER>();
+        fragments((Q + 1) % BUFFERS, 0);
+        stage(t + BUFFERS, B, L0, L1);
         if (Q == 0) load_scales(t + 4);
         LP_STEP(Q, 3, true)
     };
 #undef LP_STEP
     if (narrow) load_narrow_scales();
     else load_scales(first);
-    stage(first, 0, L0, L3);
-    all_arrived();
-    stage(first + 1, 1, L0, L1);
+#pragma unroll
+    for (int b = 0; b < BUFFERS - 1; ++b) stage(first + b, b, L0, L3);
+    arrived_but<(BUFFERS - 2) * PER>();
+    stage(first + BUFFERS - 1, BUFFERS - 1, L0, L1);
     fragments(0, 0);
     for (int t = first;; t += 4) {
         take_scales(t);
@@ -298,6 +306,91 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
     put_results<MB, NB, OutT>(a.out, p.part, (float *)(lds + wave * result_bytes(NB)), acc, m0 + wm * MB * 32, n0 + wn * NB * 32, a.M, a.N);
 }
 
+// Few rows: the weights are all that matters, and every byte of them is read once, straight into the registers that the matrix
+// instruction (16 x 16 x 128) takes: 16 rows of w a workgroup, the reduction cut among its eight waves in chunks of 512 positions.
+// A lane holds 64 neighbouring bytes of a row in four operands, whose scale bytes are one word.  Rows of x come as codes from
+// memory, or, X a float type, are brought to codes by every wave for its own chunks: the rows are short, and a launch that
+// does it beforehand takes longer.  The waves' sums meet in LDS, added in order.
+constexpr int kFewWaves = 8;
+
+template <int RB, typename X, typename OutT>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void mx4_few_kernel(const Mx4Args a, const X *x, size_t ldx)
+{
+    constexpr bool CODES = std::is_same<X, unsigned char>::value;
+    static_assert(CODES || RB == 1, "floats: 16 rows");
+    constexpr int QROW = 256 + 16; // a quantized row of a chunk in LDS: codes, scale bytes
+    __shared__ __align__(16) unsigned char lds[CODES ? 16 : kFewWaves * 16 * QROW];
+    __shared__ __align__(32) float sums[kFewWaves][RB * 16][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, q = lane >> 4;
+    const int n0 = blockIdx.x * 16, chunks = (a.blocks + 15) / 16;
+    const unsigned pitch = (unsigned)a.blocks * 16;
+    // rows beyond the last lie outside the descriptors, and so is what lies behind a row: zeros
+    const int wrows = min(a.N - n0, 16);
+    const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.wc) + (size_t)n0 * pitch, 0, wrows * pitch, 0x00020000);
+    const __amdgpu_buffer_rsrc_t wsr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.ws) + (size_t)n0 * a.blocks, 0, wrows * a.blocks, 0x00020000);
+    const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.xc), 0, CODES ? a.M * pitch : 0, 0x00020000);
+    const __amdgpu_buffer_rsrc_t xsr = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.xs), 0, CODES ? a.M * a.blocks : 0, 0x00020000);
+    struct Operand {
+        v4i f[4];
+        int s;
+    };
+    auto load = [&](Operand &o, __amdgpu_buffer_rsrc_t codes, __amdgpu_buffer_rsrc_t scales, int row, int chunk) __attribute__((always_inline)) {
+        const unsigned block = row * (unsigned)a.blocks + 16 * chunk + 4 * q;
+        const bool there = 16 * chunk + 4 * q < a.blocks;
+        const unsigned at = there ? block * 16 : 0xfffffff0u - 64;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o.f[k] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(codes, at + 16 * k, 0, 0));
+        o.s = __builtin_amdgcn_raw_buffer_load_b32(scales, there ? block : 0xfffffff0u, 0, 0);
+    };
+    v4f acc[RB] = {};
+    Operand w, xo[RB];
+    auto products = [&]() __attribute__((always_inline)) {
+#define LP_PART(S)                                                                                                                          \
+    _Pragma("unroll") for (int b = 0; b < RB; ++b)                                                                                           \
+    {                                                                                                                                       \
+        const v8i u = {w.f[S][0], w.f[S][1], w.f[S][2], w.f[S][3], 0, 0, 0, 0}, v = {xo[b].f[S][0], xo[b].f[S][1], xo[b].f[S][2], xo[b].f[S][3], 0, 0, 0, 0}; \
+        acc[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v, acc[b], 4, 4, S, w.s, S, xo[b].s);                                  \
+    }
+        LP_PART(0)
+        LP_PART(1)
+        LP_PART(2)
+        LP_PART(3)
+#undef LP_PART
+    };
+    for (int c = wave; c < chunks; c += kFewWaves) {
+        load(w, wr, wsr, r16, c);
+        if constexpr (CODES) {
+#pragma unroll
+            for (int b = 0; b < RB; ++b) load(xo[b], xr, xsr, b * 16 + r16, c);
+        } else {
+            unsigned char *mine = lds + wave * 16 * QROW;
+            const int at = c * 512 + lane * 8, n = (int)a.K - at;
+#pragma unroll 4
+            for (int r = 0; r < a.M; ++r) {
+                const v8f v = load8(x + r * ldx + at, n);
+                const int e = mx4_scale_byte(block_exponent(v));
+                *(unsigned *)(mine + r * QROW + lane * 4) = mx4_word(v, e);
+                if ((lane & 3) == 0) mine[r * QROW + 256 + lane / 4] = (unsigned char)e;
+            }
+            const int row = min(r16, a.M - 1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) xo[0].f[k] = *(const v4i *)(mine + row * QROW + (4 * q + k) * 16);
+            xo[0].s = *(const int *)(mine + row * QROW + 256 + 4 * q);
+        }
+        products();
+    }
+#pragma unroll
+    for (int b = 0; b < RB; ++b) *(v4f *)&sums[wave][b * 16 + r16][4 * q] = acc[b];
+    __syncthreads();
+    const int m = threadIdx.x / 2, n = n0 + threadIdx.x % 2 * 8;
+    if (m < RB * 16 && m < a.M && n < a.N) {
+        v8f v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kFewWaves; ++k) v += *(const v8f *)&sums[k][m][n - n0];
+        put8(a.out, (OutT *)a.out.y + m * a.out.ld + n, a.out.bias + n, a.N - n, v);
+    }
+}
+
 // -------------------------------------------------------------------------------- gradients
 
 // D[i][j] = sum_c A(i, c) B(c, j) on v_mfma_f32_32x32x16_bf16, A the bfloat16 gradient dY, B an mx4 or ckpt8 tensor whose rows are
@@ -305,13 +398,13 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
 //   gradient of the input:    i = m, c = n, j = k; A(i, c) = dY[i][c], B = Wq
 //   gradient of the weights:  i = n, c = m, j = k; A(i, c) = dY[c][i], B = X8
 //
-// A workgroup owns TI x TJ results, a wave MB x NB blocks of 32 x 32; a stage is 64 positions of the reduction in one of two LDS
-// buffers.  B's codes pass through registers, a block of 32 a thread, loaded two stages ahead, decoded one stage ahead; dY
+// A workgroup owns TI x TJ results, a wave MB x NB blocks of 32 x 32; a stage is 64 positions of the reduction in one of BUFFERS
+// LDS buffers.  B's codes pass through registers, a block of 32 a thread, and are decoded one stage ahead; dY
 // comes by loads to LDS (or, where its rows do not start on words, through registers like the codes).  The matrix
 // instruction wants eight neighbouring positions of a row or column in a lane: those of dY's rows lie together in memory
 // (16-byte piece p of row r at place p ^ (r % 8), as above); tiles with the reduction along their rows are read by
 // ds_read_b64_tr_b16, which hands each of 16 lanes four rows' elements of its column.  Their rows are 512 (or 256) bytes, so
-// the four rows of such a read lie in the same banks unless the 64-byte pieces of row r change places with r % 4.  Decoded
+// the four rows of such a read lie in the same banks unless the 64-byte pieces of row r change places with r % 4 (r % 2 where a row has two).  Decoded
 // codes also swap neighbouring 16 bytes where (column / 128 + row) is odd, for the sake of the writes.
 //
 // B is the row operand of the instruction, so that a lane ends up with four neighbouring columns of one row of D.
@@ -395,15 +488,18 @@ struct RawBlock {
     }
 };
 
-template <int MB, int NB, int WM, int WN, bool WEIGHTS, bool WORDS, typename OutT>
+template <int MB, int NB, int WM, int WN, int BUFFERS, bool WEIGHTS, bool WORDS, typename OutT>
 __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs a)
 {
+    static_assert(BUFFERS == 2 || BUFFERS == 4, "a stage's buffer is known where it is written out");
     constexpr int TI = MB * 32 * WM, TJ = NB * 32 * WN, WAVES = WM * WN, THREADS = WAVES * 64;
     constexpr int ABYTES = TI * 128, BBYTES = TJ * 128, STAGE = ABYTES + BBYTES;
     constexpr int PER = ABYTES / 1024 / WAVES; // a wave's loads of dY per stage, and a thread's pieces
     constexpr int AROW = WEIGHTS ? TI * 2 : 128, BROW = TJ * 2;
+    constexpr int ATURN = (AROW < 256 ? AROW / 64 : 4) - 1, BTURN = (BROW < 256 ? BROW / 64 : 4) - 1; // 64-byte pieces that change places
+    static_assert((AROW & (AROW - 1)) == 0 && (BROW & (BROW - 1)) == 0, "places are exchanged within a row");
     static_assert(TJ * 2 == THREADS, "a thread decodes one block of 32 per stage");
-    __shared__ __align__(1024) unsigned char lds[2 * STAGE];
+    __shared__ __align__(1024) unsigned char lds[BUFFERS * STAGE];
     static_assert(WAVES * result_bytes(NB) <= (int)sizeof(lds), "results pass through the same memory");
     Place p;
     if (!find_place(a.grid, &p)) return;
@@ -421,7 +517,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
         if constexpr (WEIGHTS) {
             constexpr int LANES = AROW / 16; // of a row
             const int r = (wave * PER + q) * (64 / LANES) + lane / LANES, s = lane % LANES;
-            at[q] = (unsigned)r * (unsigned)(a.ld * 2) + (((s >> 2) ^ (r & 3)) * 4 + (s & 3)) * 16;
+            at[q] = (unsigned)r * (unsigned)(a.ld * 2) + (((s >> 2) ^ (r & ATURN)) * 4 + (s & 3)) * 16;
         } else {
             const int r = (wave * PER + q) * 8 + lane / 8;
             at[q] = (unsigned)min(r, a.I - 1 - i0) * (unsigned)(a.ld * 2) + ((lane & 7) ^ (r & 7)) * 16;
@@ -430,8 +526,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     // loads FROM .. TO - 1 of a wave's share of stage t; where nothing is to come the descriptor is empty and zeros arrive
     auto load_dy = [&](int t, int buf, auto from, auto to) __attribute__((always_inline)) {
         if constexpr (WORDS) {
-            const int size = __builtin_amdgcn_readfirstlane(t < whole ? -1 : 0);
             const __bf16 *base = WEIGHTS ? a.dy + (size_t)t * 64 * a.ld + i0 : a.dy + (size_t)i0 * a.ld + t * 64;
+            // Weights: a tile's row may reach past the end of dY's, over several of them where these are short; not past the last
+            // one's.  (Whole words: the last row is not brought this way.)
+            const long long rest = ((long long)(a.C - 1 - t * 64) * (long long)a.ld + (a.I - i0)) * 2;
+            const int all = WEIGHTS ? (int)(unsigned)std::min(rest & ~3LL, 0xfffffffcLL) : -1;
+            const int size = __builtin_amdgcn_readfirstlane(t < whole ? all : 0);
             const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16 *>(base), 0, size, 0x00020000);
 #pragma unroll
             for (int q = decltype(from)::value; q < decltype(to)::value; ++q) load_lds16(rsrc, lds + buf * STAGE + (wave * PER + q) * 1024, at[q], 0);
@@ -447,46 +547,58 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
             raw_dy[q] = load_piece(a.dy + row * a.ld + col, row < rows && t < last ? cols - col : 0);
         }
     };
+    // the same at once, a piece at a time
+    auto bring_dy = [&](int t, int buf) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int k = threadIdx.x; k < PER * THREADS; k += THREADS) {
+            const int r = k / (AROW / 16), s = k % (AROW / 16), to = WEIGHTS ? ((s >> 2) ^ (r & ATURN)) * 4 + (s & 3) : s ^ (r & 7);
+            const int row = WEIGHTS ? t * 64 + r : i0 + r, col = WEIGHTS ? i0 + s * 8 : t * 64 + s * 8;
+            const v4u piece = load_piece(a.dy + row * a.ld + col, row < (WEIGHTS ? a.C : a.I) ? (WEIGHTS ? a.I : a.C) - col : 0);
+            __builtin_amdgcn_s_waitcnt(0); // (and the zeros of the empty loads have arrived)
+            *(v4u *)(lds + buf * STAGE + r * AROW + to * 16) = piece;
+        }
+    };
     auto place_dy = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int q = 0; q < PER; ++q) {
             const int k = q * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
-            const int to = WEIGHTS ? ((s >> 2) ^ (r & 3)) * 4 + (s & 3) : s ^ (r & 7);
+            const int to = WEIGHTS ? ((s >> 2) ^ (r & ATURN)) * 4 + (s & 3) : s ^ (r & 7);
             *(v4u *)(lds + buf * STAGE + r * AROW + to * 16) = raw_dy[q];
         }
     };
 
     // B: thread's row of the stage and block of the row.  The descriptors start at a stage's first row and end with the tensor.
-    RawBlock<WEIGHTS> raw;
+    constexpr int RAW = BUFFERS == 4 ? 4 : 1; // blocks of a thread on their way
+    RawBlock<WEIGHTS> raw[RAW];
     const int brow = threadIdx.x / (TJ / 32), bblock = threadIdx.x % (TJ / 32);
     const unsigned bat = j0 / 32 + bblock < a.blocks ? (unsigned)brow * (unsigned)a.blocks + (unsigned)(j0 / 32 + bblock) : 0x07ffffffu;
     // (eight lanes that write together hold one piece of each 64 bytes of a row, or of two rows: half of them swap neighbours)
-    unsigned char *const bplace = lds + ABYTES + brow * BROW + (bblock ^ (brow & 3)) * 64;
+    unsigned char *const bplace = lds + ABYTES + brow * BROW + (bblock ^ (brow & BTURN)) * 64;
     const int bswap = ((bblock >> 2 ^ brow) & 1) * 16;
     const int end = min(last * 64, a.C);
-    auto load_b = [&](int t) __attribute__((always_inline)) {
+    auto load_b = [&](int t, int r) __attribute__((always_inline)) {
         constexpr int BLOCK = WEIGHTS ? 32 : 16;
         const long long left = std::min(std::max((long long)(end - t * 64) * a.blocks, 0LL), 0x07ffffffLL); // blocks
         const int scales = __builtin_amdgcn_readfirstlane((int)left), codes = scales * BLOCK;
         const size_t from = (size_t)t * 64 * a.blocks;
-        raw.load(__builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.codes) + from * BLOCK, 0, codes, 0x00020000),
+        raw[r].load(__builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.codes) + from * BLOCK, 0, codes, 0x00020000),
                  __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.scales) + from, 0, scales, 0x00020000), bat);
     };
-    auto place_b = [&](int buf, int from, int to) __attribute__((always_inline)) {
+    auto place_b = [&](int r, int buf, int from, int to) __attribute__((always_inline)) {
 #pragma unroll
-        for (int k = from; k < to; ++k) *(v4u *)(bplace + buf * STAGE + (k * 16 ^ bswap)) = raw.piece(k);
+        for (int k = from; k < to; ++k) *(v4u *)(bplace + buf * STAGE + (k * 16 ^ bswap)) = raw[r].piece(k);
     };
 
     v16f acc[NB][MB] = {};
     v8s fa[2][MB], fb[2][NB];
     // this lane's place in a read of four rows x 16 columns (x0: the tile column of its block of 32)
     const int tr_row = 8 * h + (lane & 15) / 4, tr_col = (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-    auto tr_place = [&](int x0, int row_bytes) __attribute__((always_inline)) { return tr_row * row_bytes + ((x0 / 32) ^ (tr_row & 3)) * 64 + tr_col; };
+    auto tr_place = [&](int x0, int row_bytes, int turn) __attribute__((always_inline)) { return tr_row * row_bytes + ((x0 / 32) ^ (tr_row & turn)) * 64 + tr_col; };
     int apos[MB], bpos[NB];
 #pragma unroll
-    for (int b = 0; b < MB; ++b) apos[b] = WEIGHTS ? tr_place((wm * MB + b) * 32, AROW) : ((wm * MB + b) * 32 + l32) * 128;
+    for (int b = 0; b < MB; ++b) apos[b] = WEIGHTS ? tr_place((wm * MB + b) * 32, AROW, ATURN) : ((wm * MB + b) * 32 + l32) * 128;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) bpos[b] = ABYTES + (tr_place((wn * NB + b) * 32, BROW) ^ (((wn * NB + b) >> 2 ^ tr_row) & 1) * 16);
+    for (int b = 0; b < NB; ++b) bpos[b] = ABYTES + (tr_place((wn * NB + b) * 32, BROW, BTURN) ^ (((wn * NB + b) >> 2 ^ tr_row) & 1) * 16);
     auto tr_read = [&](int pos, int row_bytes) __attribute__((always_inline)) { return read_columns(lds + pos, lds + pos + 4 * row_bytes); };
     auto fragments = [&](int buf, int s) __attribute__((always_inline)) {
 #pragma unroll
@@ -528,52 +640,53 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     constexpr std::integral_constant<int, 0> L0;
     constexpr std::integral_constant<int, PER / 2> L1;
     constexpr std::integral_constant<int, PER> L2;
-    // Stage t in buffer B: while it is multiplied the next one is completed in the other buffer.
-    auto whole_stage = [&](int t, auto buffer) __attribute__((always_inline)) {
-        constexpr int B = decltype(buffer)::value;
+    // Stage t, number Q of its four from the first on: while it is multiplied the next one is decoded, the loads that a register or a
+    // buffer became free for are asked for.
+    auto whole_stage = [&](int t, auto number) __attribute__((always_inline)) {
+        constexpr int Q = decltype(number)::value, B = Q % BUFFERS, NEXT = (Q + 1) % BUFFERS, BEFORE = (Q + BUFFERS - 1) % BUFFERS, R = (Q + 1) % RAW;
+        // loads that may still be on their way when the next stage's dY has arrived: those of the stages behind it
+        constexpr int LATER = WORDS ? (BUFFERS - 2) * PER + (BUFFERS - 1) * (WEIGHTS ? 3 : 2) : 0;
         __builtin_amdgcn_sched_barrier(0);
         fragments(B, 1);
-        load_dy(t + 1, B ^ 1, L1, L2);
-        place_b(B ^ 1, 0, 2);
+        load_dy(t + BUFFERS - 1, BEFORE, L1, L2);
+        place_b(R, NEXT, 0, 2);
         LP_STEP(0)
         fragments(B, 2);
-        place_b(B ^ 1, 2, 4);
-        load_b(t + 2);
+        place_b(R, NEXT, 2, 4);
+        load_b(t + 1 + RAW, R);
         LP_STEP(1)
         if constexpr (!WORDS) {
-            place_dy(B ^ 1);
+            place_dy(NEXT);
             fetch_dy(t + 2);
         }
         fragments(B, 3);
         LP_STEP(2)
-        if (WORDS && ragged && t + 2 == last) {
-            fetch_dy(t + 1);
-            __builtin_amdgcn_s_waitcnt(0); // (and the zeros of the empty loads have arrived)
-            place_dy(B ^ 1);
-        }
-        all_arrived();
-        fragments(B ^ 1, 0);
-        load_dy(t + 2, B, L0, L1);
+        if (WORDS && ragged && t + 2 == last) bring_dy(t + 1, NEXT);
+        arrived_but<LATER>();
+        fragments(NEXT, 0);
+        load_dy(t + BUFFERS, B, L0, L1);
         LP_STEP(3)
     };
-    load_b(first);
-    load_dy(first, 0, L0, L2);
-    place_b(0, 0, 4);
-    load_b(first + 1);
-    if (!WORDS || whole == first) {
-        fetch_dy(first);
-        __builtin_amdgcn_s_waitcnt(0);
-        place_dy(0);
-    }
+#pragma unroll
+    for (int r = 0; r < RAW; ++r) load_b(first + r, r);
+#pragma unroll
+    for (int b = 0; b < BUFFERS - 1; ++b) load_dy(first + b, b, L0, L2);
+    place_b(0, 0, 0, 4);
+    load_b(first + RAW, 0);
+    if (!WORDS || whole == first) bring_dy(first, 0);
     if constexpr (!WORDS) fetch_dy(first + 1);
     all_arrived();
-    load_dy(first + 1, 1, L0, L1);
+    load_dy(first + BUFFERS - 1, BUFFERS - 1, L0, L1);
     fragments(0, 0);
-    for (int t = first;; t += 2) {
+    for (int t = first;; t += 4) {
         whole_stage(t, std::integral_constant<int, 0>());
         if (t + 1 >= last) break;
         whole_stage(t + 1, std::integral_constant<int, 1>());
         if (t + 2 >= last) break;
+        whole_stage(t + 2, std::integral_constant<int, 2>());
+        if (t + 3 >= last) break;
+        whole_stage(t + 3, std::integral_constant<int, 3>());
+        if (t + 4 >= last) break;
     }
 #undef LP_STEP
     all_arrived();
@@ -650,7 +763,13 @@ static void join_parts(const float *sums, int parts, size_t part, size_t ldp, lp
     });
 }
 
+constexpr int kFewRows = 64;
+// Rows of x times chunks a wave: up to here every workgroup quantizes for itself.
+constexpr size_t kFewFloats = 8;
+
 struct Mx4Plan {
+    int few;              // few rows: the kernel for them, with this many blocks of 16 rows; 0: tiles
+    bool floats;          // it takes x as floats
     Cut cut;
     size_t blocks;        // of 32 per row
     size_t codes, scales; // workspace: quantized x (if the call brings floats), then the sums of the parts
@@ -661,7 +780,10 @@ static Mx4Plan mx4_plan(int M, int K, int Nout)
 {
     Mx4Plan p = {};
     p.blocks = mx4_blocks((size_t)K);
-    p.cut = cut_product(M, Nout, (int)(p.blocks / 8), 4, 4);
+    p.few = M <= kFewRows ? (M + 15) / 16 : 0;
+    p.floats = M * ((p.blocks + 16 * kFewWaves - 1) / (16 * kFewWaves)) <= kFewFloats;
+    if (p.floats) return p;
+    if (!p.few) p.cut = cut_product(M, Nout, (int)(p.blocks / 8), 4, 4);
     p.codes = round256((size_t)M * p.blocks * 16);
     p.scales = round256((size_t)M * p.blocks);
     return p;
@@ -671,8 +793,26 @@ template <typename T>
 static void mx4_launch(const Cut &c, const Mx4Args &a, hipStream_t st)
 {
     const dim3 grid((unsigned)a.grid.per_xcd * kXCDs);
-    if (c.large) hipLaunchKernelGGL((mx4_product_kernel<4, 2, 2, 4, T>), grid, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((mx4_product_kernel<2, 2, 2, 2, T>), grid, dim3(256), 0, st, a);
+    if (c.large) hipLaunchKernelGGL((mx4_product_kernel<4, 2, 2, 4, 2, T>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((mx4_product_kernel<2, 2, 2, 2, 2, T>), grid, dim3(256), 0, st, a);
+}
+
+template <typename T>
+static void few_launch(const Mx4Plan &p, const Mx4Args &a, const void *x, lp_dtype xt, size_t ldx, hipStream_t st)
+{
+    const dim3 grid((unsigned)((a.N + 15) / 16)), block(kFewWaves * 64);
+    const unsigned char *none = nullptr;
+    if (a.xs) {
+        if (p.few == 1) hipLaunchKernelGGL((mx4_few_kernel<1, unsigned char, T>), grid, block, 0, st, a, none, ldx);
+        else if (p.few == 2) hipLaunchKernelGGL((mx4_few_kernel<2, unsigned char, T>), grid, block, 0, st, a, none, ldx);
+        else if (p.few == 3) hipLaunchKernelGGL((mx4_few_kernel<3, unsigned char, T>), grid, block, 0, st, a, none, ldx);
+        else hipLaunchKernelGGL((mx4_few_kernel<4, unsigned char, T>), grid, block, 0, st, a, none, ldx);
+    } else {
+        with_type(xt, [&](auto *tag) {
+            typedef std::remove_pointer_t<decltype(tag)> X;
+            hipLaunchKernelGGL((mx4_few_kernel<1, X, T>), grid, block, 0, st, a, (const X *)x, ldx);
+        });
+    }
 }
 
 // Gradients: workspace of the parts' sums, then of the bias's.
@@ -697,11 +837,11 @@ static void grad_launch(const Cut &c, const GradArgs &a, hipStream_t st)
     // Loads to LDS ask for words, and reach 2^31 bytes from a tile's first row.
     const bool words = aligned_to(a.dy, 4) && a.ld % 2 == 0 && a.ld < ((size_t)1 << 22);
     if (c.large) {
-        if (words) hipLaunchKernelGGL((gradient_kernel<4, 2, 2, 4, WEIGHTS, true, T>), grid, dim3(512), 0, st, a);
-        else hipLaunchKernelGGL((gradient_kernel<4, 2, 2, 4, WEIGHTS, false, T>), grid, dim3(512), 0, st, a);
+        if (words) hipLaunchKernelGGL((gradient_kernel<4, 2, 2, 4, 2, WEIGHTS, true, T>), grid, dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((gradient_kernel<4, 2, 2, 4, 2, WEIGHTS, false, T>), grid, dim3(512), 0, st, a);
     } else {
-        if (words) hipLaunchKernelGGL((gradient_kernel<2, 2, 2, 2, WEIGHTS, true, T>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((gradient_kernel<2, 2, 2, 2, WEIGHTS, false, T>), grid, dim3(256), 0, st, a);
+        if (words) hipLaunchKernelGGL((gradient_kernel<2, 2, 2, 2, 2, WEIGHTS, true, T>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((gradient_kernel<2, 2, 2, 2, 2, WEIGHTS, false, T>), grid, dim3(256), 0, st, a);
     }
 }
 
@@ -772,15 +912,19 @@ extern "C" lp_status lp_mx4_fc_fwd(int M, int K, int Nout, const void *x_dev, lp
     a.ws = (const unsigned char *)w_scales_dev;
     a.M = M;
     a.N = Nout;
+    a.K = K;
     a.blocks = (int)p.blocks;
     a.grid = p.cut.grid;
-    if (!a.xs) {
+    if (!a.xs && !p.floats) {
         mx4_quantize_launch(x_dev, xt, (size_t)M, (size_t)K, ldx, work, work + p.codes, st);
         a.xc = work;
         a.xs = work + p.codes;
     }
     const Sink out{y_dev, ldy, 0, bias_dev, act, 0};
-    if (a.grid.parts > 1) {
+    if (p.few) {
+        a.out = out;
+        with_type(yt, [&](auto *tag) { few_launch<std::remove_pointer_t<decltype(tag)>>(p, a, x_dev, xt, ldx, st); });
+    } else if (a.grid.parts > 1) {
         float *sums = (float *)(work + p.codes + p.scales);
         const size_t part = (size_t)M * p.cut.ldp;
         a.out = Sink{sums, p.cut.ldp, part, nullptr, LP_ACT_NONE, 0};

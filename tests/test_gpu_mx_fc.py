@@ -157,7 +157,7 @@ def check_wgrad(m, k, n, dwt, with_bias, accumulate=False, extra=-1):
     junk_is_left(wide, k)
 
 
-@pytest.mark.parametrize("size", SIZES + [(0, 70, 40), (4000, 200, 136)])
+@pytest.mark.parametrize("size", SIZES + [(0, 70, 40), (4000, 200, 136), (1000, 64, 2), (300, 500, 6), (129, 33, 1)])
 def test_weight_gradient(size):
     check_wgrad(*size, torch.float32, True)
     check_wgrad(*size, torch.bfloat16, True, accumulate=True, extra=3)
