@@ -306,21 +306,20 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
     put_results<MB, NB, OutT>(a.out, p.part, (float *)(lds + wave * result_bytes(NB)), acc, m0 + wm * MB * 32, n0 + wn * NB * 32, a.M, a.N);
 }
 
-// Few rows: the weights are all that matters, and every byte of them is read once, straight into the registers that the matrix
+// Few rows (16 at most): the weights are all that matters, and every byte of them is read once, straight into the registers that the matrix
 // instruction (16 x 16 x 128) takes: 16 rows of w a workgroup, the reduction cut among its eight waves in chunks of 512 positions.
 // A lane holds 64 neighbouring bytes of a row in four operands, whose scale bytes are one word.  Rows of x come as codes from
 // memory, or, X a float type, are brought to codes by every wave for its own chunks: the rows are short, and a launch that
 // does it beforehand takes longer.  The waves' sums meet in LDS, added in order.
 constexpr int kFewWaves = 8;
 
-template <int RB, typename X, typename OutT>
+template <typename X, typename OutT>
 __global__ __launch_bounds__(kFewWaves * 64, 2) void mx4_few_kernel(const Mx4Args a, const X *x, size_t ldx)
 {
     constexpr bool CODES = std::is_same<X, unsigned char>::value;
-    static_assert(CODES || RB == 1, "floats: 16 rows");
     constexpr int QROW = 256 + 16; // a quantized row of a chunk in LDS: codes, scale bytes
     __shared__ __align__(16) unsigned char lds[CODES ? 16 : kFewWaves * 16 * QROW];
-    __shared__ __align__(32) float sums[kFewWaves][RB * 16][16];
+    __shared__ __align__(32) float sums[kFewWaves][16][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, q = lane >> 4;
     const int n0 = blockIdx.x * 16, chunks = (a.blocks + 15) / 16;
     const unsigned pitch = (unsigned)a.blocks * 16;
@@ -342,52 +341,44 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void mx4_few_kernel(const Mx4Arg
         for (int k = 0; k < 4; ++k) o.f[k] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(codes, at + 16 * k, 0, 0));
         o.s = __builtin_amdgcn_raw_buffer_load_b32(scales, there ? block : 0xfffffff0u, 0, 0);
     };
-    v4f acc[RB] = {};
-    Operand w, xo[RB];
-    auto products = [&]() __attribute__((always_inline)) {
+    v4f acc = 0.0f;
+    Operand w, v;
 #define LP_PART(S)                                                                                                                          \
-    _Pragma("unroll") for (int b = 0; b < RB; ++b)                                                                                           \
-    {                                                                                                                                       \
-        const v8i u = {w.f[S][0], w.f[S][1], w.f[S][2], w.f[S][3], 0, 0, 0, 0}, v = {xo[b].f[S][0], xo[b].f[S][1], xo[b].f[S][2], xo[b].f[S][3], 0, 0, 0, 0}; \
-        acc[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v, acc[b], 4, 4, S, w.s, S, xo[b].s);                                  \
-    }
-        LP_PART(0)
-        LP_PART(1)
-        LP_PART(2)
-        LP_PART(3)
-#undef LP_PART
-    };
+    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v8i{w.f[S][0], w.f[S][1], w.f[S][2], w.f[S][3], 0, 0, 0, 0},                     \
+                                                           v8i{v.f[S][0], v.f[S][1], v.f[S][2], v.f[S][3], 0, 0, 0, 0}, acc, 4, 4, S, w.s, S, v.s);
     for (int c = wave; c < chunks; c += kFewWaves) {
         load(w, wr, wsr, r16, c);
         if constexpr (CODES) {
-#pragma unroll
-            for (int b = 0; b < RB; ++b) load(xo[b], xr, xsr, b * 16 + r16, c);
+            load(v, xr, xsr, r16, c);
         } else {
             unsigned char *mine = lds + wave * 16 * QROW;
             const int at = c * 512 + lane * 8, n = (int)a.K - at;
 #pragma unroll 4
             for (int r = 0; r < a.M; ++r) {
-                const v8f v = load8(x + r * ldx + at, n);
-                const int e = mx4_scale_byte(block_exponent(v));
-                *(unsigned *)(mine + r * QROW + lane * 4) = mx4_word(v, e);
+                const v8f f = load8(x + r * ldx + at, n);
+                const int e = mx4_scale_byte(block_exponent(f));
+                *(unsigned *)(mine + r * QROW + lane * 4) = mx4_word(f, e);
                 if ((lane & 3) == 0) mine[r * QROW + 256 + lane / 4] = (unsigned char)e;
             }
             const int row = min(r16, a.M - 1);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) xo[0].f[k] = *(const v4i *)(mine + row * QROW + (4 * q + k) * 16);
-            xo[0].s = *(const int *)(mine + row * QROW + 256 + 4 * q);
+            for (int k = 0; k < 4; ++k) v.f[k] = *(const v4i *)(mine + row * QROW + (4 * q + k) * 16);
+            v.s = *(const int *)(mine + row * QROW + 256 + 4 * q);
         }
-        products();
+        LP_PART(0)
+        LP_PART(1)
+        LP_PART(2)
+        LP_PART(3)
     }
-#pragma unroll
-    for (int b = 0; b < RB; ++b) *(v4f *)&sums[wave][b * 16 + r16][4 * q] = acc[b];
+#undef LP_PART
+    *(v4f *)&sums[wave][r16][4 * q] = acc;
     __syncthreads();
     const int m = threadIdx.x / 2, n = n0 + threadIdx.x % 2 * 8;
-    if (m < RB * 16 && m < a.M && n < a.N) {
-        v8f v = 0.0f;
+    if (m < 16 && m < a.M && n < a.N) {
+        v8f sum = 0.0f;
 #pragma unroll
-        for (int k = 0; k < kFewWaves; ++k) v += *(const v8f *)&sums[k][m][n - n0];
-        put8(a.out, (OutT *)a.out.y + m * a.out.ld + n, a.out.bias + n, a.N - n, v);
+        for (int k = 0; k < kFewWaves; ++k) sum += *(const v8f *)&sums[k][m][n - n0];
+        put8(a.out, (OutT *)a.out.y + m * a.out.ld + n, a.out.bias + n, a.N - n, sum);
     }
 }
 
@@ -398,7 +389,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void mx4_few_kernel(const Mx4Arg
 //   gradient of the input:    i = m, c = n, j = k; A(i, c) = dY[i][c], B = Wq
 //   gradient of the weights:  i = n, c = m, j = k; A(i, c) = dY[c][i], B = X8
 //
-// A workgroup owns TI x TJ results, a wave MB x NB blocks of 32 x 32; a stage is 64 positions of the reduction in one of BUFFERS
+// A workgroup owns TI x TJ results, a wave MB x NB blocks of 32 x 32; a stage is 64 positions of the reduction in one of two
 // LDS buffers.  B's codes pass through registers, a block of 32 a thread, and are decoded one stage ahead; dY
 // comes by loads to LDS (or, where its rows do not start on words, through registers like the codes).  The matrix
 // instruction wants eight neighbouring positions of a row or column in a lane: those of dY's rows lie together in memory
@@ -488,10 +479,9 @@ struct RawBlock {
     }
 };
 
-template <int MB, int NB, int WM, int WN, int BUFFERS, bool WEIGHTS, bool WORDS, typename OutT>
+template <int MB, int NB, int WM, int WN, bool WEIGHTS, bool WORDS, typename OutT>
 __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs a)
 {
-    static_assert(BUFFERS == 2 || BUFFERS == 4, "a stage's buffer is known where it is written out");
     constexpr int TI = MB * 32 * WM, TJ = NB * 32 * WN, WAVES = WM * WN, THREADS = WAVES * 64;
     constexpr int ABYTES = TI * 128, BBYTES = TJ * 128, STAGE = ABYTES + BBYTES;
     constexpr int PER = ABYTES / 1024 / WAVES; // a wave's loads of dY per stage, and a thread's pieces
@@ -499,7 +489,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     constexpr int ATURN = (AROW < 256 ? AROW / 64 : 4) - 1, BTURN = (BROW < 256 ? BROW / 64 : 4) - 1; // 64-byte pieces that change places
     static_assert((AROW & (AROW - 1)) == 0 && (BROW & (BROW - 1)) == 0, "places are exchanged within a row");
     static_assert(TJ * 2 == THREADS, "a thread decodes one block of 32 per stage");
-    __shared__ __align__(1024) unsigned char lds[BUFFERS * STAGE];
+    __shared__ __align__(1024) unsigned char lds[2 * STAGE];
     static_assert(WAVES * result_bytes(NB) <= (int)sizeof(lds), "results pass through the same memory");
     Place p;
     if (!find_place(a.grid, &p)) return;
@@ -568,25 +558,24 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     };
 
     // B: thread's row of the stage and block of the row.  The descriptors start at a stage's first row and end with the tensor.
-    constexpr int RAW = BUFFERS == 4 ? 4 : 1; // blocks of a thread on their way
-    RawBlock<WEIGHTS> raw[RAW];
+    RawBlock<WEIGHTS> raw;
     const int brow = threadIdx.x / (TJ / 32), bblock = threadIdx.x % (TJ / 32);
     const unsigned bat = j0 / 32 + bblock < a.blocks ? (unsigned)brow * (unsigned)a.blocks + (unsigned)(j0 / 32 + bblock) : 0x07ffffffu;
     // (eight lanes that write together hold one piece of each 64 bytes of a row, or of two rows: half of them swap neighbours)
     unsigned char *const bplace = lds + ABYTES + brow * BROW + (bblock ^ (brow & BTURN)) * 64;
     const int bswap = ((bblock >> 2 ^ brow) & 1) * 16;
     const int end = min(last * 64, a.C);
-    auto load_b = [&](int t, int r) __attribute__((always_inline)) {
+    auto load_b = [&](int t) __attribute__((always_inline)) {
         constexpr int BLOCK = WEIGHTS ? 32 : 16;
         const long long left = std::min(std::max((long long)(end - t * 64) * a.blocks, 0LL), 0x07ffffffLL); // blocks
         const int scales = __builtin_amdgcn_readfirstlane((int)left), codes = scales * BLOCK;
         const size_t from = (size_t)t * 64 * a.blocks;
-        raw[r].load(__builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.codes) + from * BLOCK, 0, codes, 0x00020000),
+        raw.load(__builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.codes) + from * BLOCK, 0, codes, 0x00020000),
                  __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.scales) + from, 0, scales, 0x00020000), bat);
     };
-    auto place_b = [&](int r, int buf, int from, int to) __attribute__((always_inline)) {
+    auto place_b = [&](int buf, int from, int to) __attribute__((always_inline)) {
 #pragma unroll
-        for (int k = from; k < to; ++k) *(v4u *)(bplace + buf * STAGE + (k * 16 ^ bswap)) = raw[r].piece(k);
+        for (int k = from; k < to; ++k) *(v4u *)(bplace + buf * STAGE + (k * 16 ^ bswap)) = raw.piece(k);
     };
 
     v16f acc[NB][MB] = {};
@@ -640,53 +629,46 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     constexpr std::integral_constant<int, 0> L0;
     constexpr std::integral_constant<int, PER / 2> L1;
     constexpr std::integral_constant<int, PER> L2;
-    // Stage t, number Q of its four from the first on: while it is multiplied the next one is decoded, the loads that a register or a
-    // buffer became free for are asked for.
-    auto whole_stage = [&](int t, auto number) __attribute__((always_inline)) {
-        constexpr int Q = decltype(number)::value, B = Q % BUFFERS, NEXT = (Q + 1) % BUFFERS, BEFORE = (Q + BUFFERS - 1) % BUFFERS, R = (Q + 1) % RAW;
-        // loads that may still be on their way when the next stage's dY has arrived: those of the stages behind it
-        constexpr int LATER = WORDS ? (BUFFERS - 2) * PER + (BUFFERS - 1) * (WEIGHTS ? 3 : 2) : 0;
+    // Stage t in buffer B: while it is multiplied the next one is completed in the other buffer.
+    auto whole_stage = [&](int t, auto buffer) __attribute__((always_inline)) {
+        constexpr int B = decltype(buffer)::value;
+        // loads that may still be on their way when the next stage's dY has arrived: the codes of the one behind it
+        constexpr int LATER = WORDS ? (WEIGHTS ? 3 : 2) : 0;
         __builtin_amdgcn_sched_barrier(0);
         fragments(B, 1);
-        load_dy(t + BUFFERS - 1, BEFORE, L1, L2);
-        place_b(R, NEXT, 0, 2);
+        load_dy(t + 1, B ^ 1, L1, L2);
+        place_b(B ^ 1, 0, 2);
         LP_STEP(0)
         fragments(B, 2);
-        place_b(R, NEXT, 2, 4);
-        load_b(t + 1 + RAW, R);
+        place_b(B ^ 1, 2, 4);
+        load_b(t + 2);
         LP_STEP(1)
         if constexpr (!WORDS) {
-            place_dy(NEXT);
+            place_dy(B ^ 1);
             fetch_dy(t + 2);
         }
         fragments(B, 3);
         LP_STEP(2)
-        if (WORDS && ragged && t + 2 == last) bring_dy(t + 1, NEXT);
+        if (WORDS && ragged && t + 2 == last) bring_dy(t + 1, B ^ 1);
         arrived_but<LATER>();
-        fragments(NEXT, 0);
-        load_dy(t + BUFFERS, B, L0, L1);
+        fragments(B ^ 1, 0);
+        load_dy(t + 2, B, L0, L1);
         LP_STEP(3)
     };
-#pragma unroll
-    for (int r = 0; r < RAW; ++r) load_b(first + r, r);
-#pragma unroll
-    for (int b = 0; b < BUFFERS - 1; ++b) load_dy(first + b, b, L0, L2);
-    place_b(0, 0, 0, 4);
-    load_b(first + RAW, 0);
+    load_b(first);
+    load_dy(first, 0, L0, L2);
+    place_b(0, 0, 4);
+    load_b(first + 1);
     if (!WORDS || whole == first) bring_dy(first, 0);
     if constexpr (!WORDS) fetch_dy(first + 1);
     all_arrived();
-    load_dy(first + BUFFERS - 1, BUFFERS - 1, L0, L1);
+    load_dy(first + 1, 1, L0, L1);
     fragments(0, 0);
-    for (int t = first;; t += 4) {
+    for (int t = first;; t += 2) {
         whole_stage(t, std::integral_constant<int, 0>());
         if (t + 1 >= last) break;
         whole_stage(t + 1, std::integral_constant<int, 1>());
         if (t + 2 >= last) break;
-        whole_stage(t + 2, std::integral_constant<int, 2>());
-        if (t + 3 >= last) break;
-        whole_stage(t + 3, std::integral_constant<int, 3>());
-        if (t + 4 >= last) break;
     }
 #undef LP_STEP
     all_arrived();
@@ -716,32 +698,57 @@ static bool floats_ok(const void *p, lp_dtype t, size_t cols, size_t ld) { retur
 
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
+// Tiles that a product's kernel is built for, and what they cost in us: a stage of one workgroup on an idle chip and, per
+// compute unit, with all of them at work (clocks fall under full load); a first workgroup's beginning and end, what they add for
+// each further one (others of the same unit go on meanwhile).
+struct TileCost {
+    int i, j;
+    double alone, full, ends, more;
+};
+// 64 x 64, 128 x 128 (four buffers each), 256 x 256 (two); a stage is 256 positions
+constexpr TileCost kMx4Tiles[3] = {{64, 64, 0.215, 0.255, 0.7, 0.7}, {128, 128, 0.43, 0.645, 1.5, 0.3}, {256, 256, 1.25, 2.0, 1.5, 0.9}};
+// 64 x 128, 128 x 128, 256 x 256; a stage is 64 positions
+constexpr TileCost kInputTiles[3] = {{64, 128, 0.46, 0.38, 2.5, 0.25}, {128, 128, 0.56, 0.535, 3.0, 0.6}, {256, 256, 1.2, 1.75, 3.3, 2.0}};
+constexpr TileCost kWeightTiles[3] = {{64, 128, 0.48, 0.43, 2.5, 0.25}, {128, 128, 0.57, 0.645, 3.0, 0.6}, {256, 256, 1.65, 2.2, 3.3, 2.0}};
+
 // How a product I x J with `stages` stages of its reduction is cut into workgroups.
 struct Cut {
-    bool large; // tiles of 256 x 256, else 128 x 128
+    int size; // which of the tiles
     Grid grid;
     size_t ldp, sums; // the parts' sums: row length, bytes (0: one part)
+    double us;
 };
 
-static Cut cut_product(int I, int J, int stages, int step, int least)
+// The cheapest of the tiles and numbers of parts, by an estimate that the tables above were fitted to (1322 timings of 162
+// problems: the choice costs 1.2 % on the average and 20 % at most).  Results leave at 16 GB/s a compute unit; joining the
+// parts is a launch, and their sums go through memory at 6 TB/s.  A part has `step` stages or a multiple of them, and `least`
+// at least.
+static Cut cut_product(int I, int J, int stages, int step, int least, const TileCost (&tiles)[3], int out_bytes)
 {
-    Cut c = {};
-    const auto tiles = [&](int side) { return (long long)((I + side - 1) / side) * ((J + side - 1) / side); };
-    c.large = tiles(256) >= 192;
-    const int side = c.large ? 256 : 128;
-    Grid &g = c.grid;
-    g.tiles_i = (I + side - 1) / side;
-    g.tiles_j = (J + side - 1) / side;
-    g.stages = stages;
-    long long parts = 1;
-    if (!c.large) parts = std::min<long long>(std::max<long long>(2 * kCUs / std::max<long long>(tiles(side), 1), 1), std::max(stages / least, 1));
-    g.stages_per_part = (int)(((stages + parts - 1) / parts + step - 1) / step * step);
-    g.parts = (stages + g.stages_per_part - 1) / g.stages_per_part;
-    g.work = g.tiles_i * g.tiles_j * g.parts;
-    g.per_xcd = (g.work + kXCDs - 1) / kXCDs;
-    c.ldp = ((size_t)J + 7) / 8 * 8;
-    c.sums = g.parts > 1 ? round256((size_t)g.parts * I * c.ldp * 4) : 0;
-    return c;
+    Cut best = {};
+    for (int size = 0; size < 3; ++size) {
+        const TileCost &c = tiles[size];
+        const long long ti = (I + c.i - 1) / c.i, tj = (J + c.j - 1) / c.j;
+        for (int parts = 1; parts <= 32; parts += parts < 4 ? 1 : parts / 2) { // 1 2 3 4 6 9 13 19 28
+            if (parts > 1 && (stages < parts * least || ti * tj * parts > 4 * kCUs)) break;
+            const int each = ((stages + parts - 1) / parts + step - 1) / step * step, real = (stages + each - 1) / each;
+            const long long work = ti * tj * real;
+            const double rounds = (double)((work + kCUs - 1) / kCUs), busy = std::min(1.0, (double)work / kCUs);
+            const double stage = rounds > 1 ? std::max(c.alone, rounds * c.full) : c.alone + std::max(0.0, c.full - c.alone) * busy;
+            const double out = (double)c.i * c.j * (real > 1 ? 4 : out_bytes) / 16384.0 * busy;
+            double us = 2.5 + c.ends + std::min(each, stages) * stage + (rounds - 1) * c.more + rounds * out;
+            if (real > 1) us += 2.3 + (double)real * I * J * 8 / 6e6;
+            if (best.us == 0 || us < best.us) {
+                best.us = us;
+                best.size = size;
+                best.grid = Grid{(int)ti, (int)tj, stages, each, real, (int)std::min<long long>(work, 0x7fffffff), 0};
+            }
+        }
+    }
+    best.grid.per_xcd = (best.grid.work + kXCDs - 1) / kXCDs;
+    best.ldp = ((size_t)J + 7) / 8 * 8;
+    best.sums = best.grid.parts > 1 ? round256((size_t)best.grid.parts * I * best.ldp * 4) : 0;
+    return best;
 }
 
 // f(type tag) for the element type of t
@@ -763,12 +770,8 @@ static void join_parts(const float *sums, int parts, size_t part, size_t ldp, lp
     });
 }
 
-constexpr int kFewRows = 64;
-// Rows of x times chunks a wave: up to here every workgroup quantizes for itself.
-constexpr size_t kFewFloats = 8;
-
 struct Mx4Plan {
-    int few;              // few rows: the kernel for them, with this many blocks of 16 rows; 0: tiles
+    bool few;             // the kernel for few rows, else tiles
     bool floats;          // it takes x as floats
     Cut cut;
     size_t blocks;        // of 32 per row
@@ -780,10 +783,19 @@ static Mx4Plan mx4_plan(int M, int K, int Nout)
 {
     Mx4Plan p = {};
     p.blocks = mx4_blocks((size_t)K);
-    p.few = M <= kFewRows ? (M + 15) / 16 : 0;
-    p.floats = M * ((p.blocks + 16 * kFewWaves - 1) / (16 * kFewWaves)) <= kFewFloats;
+    p.cut = cut_product(M, Nout, (int)(p.blocks / 8), 4, 4, kMx4Tiles, 2);
+    if (M <= 16) {
+        // Few rows: every workgroup reads 16 rows of w and all of x, 8 TB/s in all, a wave's chunk takes half a microsecond.
+        // Quantizing x is a launch of 2.3 us, or 0.35 us a row and chunk where every wave does it.
+        // us, few rows : tiles, bf16: 1 x 4096 -> 4096 4.2 : 10, 16 rows 7.0 : 10, 16 x 4096 -> 14336 13.5 : 10.8
+        const double chunks = (double)((p.blocks + 16 * kFewWaves - 1) / (16 * kFewWaves));
+        const double read = (double)Nout * p.blocks * 17 * (1 + M / 16.0) / 8e6, few = 3.0 + std::max(0.5 * chunks, read);
+        const double within = 0.35 * M * chunks;
+        p.few = few + std::min(within, 2.3) < p.cut.us + 2.3;
+        p.floats = p.few && within < 2.8;
+    }
+    if (p.few) p.cut = Cut{};
     if (p.floats) return p;
-    if (!p.few) p.cut = cut_product(M, Nout, (int)(p.blocks / 8), 4, 4);
     p.codes = round256((size_t)M * p.blocks * 16);
     p.scales = round256((size_t)M * p.blocks);
     return p;
@@ -793,24 +805,21 @@ template <typename T>
 static void mx4_launch(const Cut &c, const Mx4Args &a, hipStream_t st)
 {
     const dim3 grid((unsigned)a.grid.per_xcd * kXCDs);
-    if (c.large) hipLaunchKernelGGL((mx4_product_kernel<4, 2, 2, 4, 2, T>), grid, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((mx4_product_kernel<2, 2, 2, 2, 2, T>), grid, dim3(256), 0, st, a);
+    if (c.size == 0) hipLaunchKernelGGL((mx4_product_kernel<1, 1, 2, 2, 4, T>), grid, dim3(256), 0, st, a);
+    else if (c.size == 1) hipLaunchKernelGGL((mx4_product_kernel<2, 2, 2, 2, 4, T>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((mx4_product_kernel<4, 2, 2, 4, 2, T>), grid, dim3(512), 0, st, a);
 }
 
 template <typename T>
-static void few_launch(const Mx4Plan &p, const Mx4Args &a, const void *x, lp_dtype xt, size_t ldx, hipStream_t st)
+static void few_launch(const Mx4Args &a, const void *x, lp_dtype xt, size_t ldx, hipStream_t st)
 {
     const dim3 grid((unsigned)((a.N + 15) / 16)), block(kFewWaves * 64);
-    const unsigned char *none = nullptr;
     if (a.xs) {
-        if (p.few == 1) hipLaunchKernelGGL((mx4_few_kernel<1, unsigned char, T>), grid, block, 0, st, a, none, ldx);
-        else if (p.few == 2) hipLaunchKernelGGL((mx4_few_kernel<2, unsigned char, T>), grid, block, 0, st, a, none, ldx);
-        else if (p.few == 3) hipLaunchKernelGGL((mx4_few_kernel<3, unsigned char, T>), grid, block, 0, st, a, none, ldx);
-        else hipLaunchKernelGGL((mx4_few_kernel<4, unsigned char, T>), grid, block, 0, st, a, none, ldx);
+        hipLaunchKernelGGL((mx4_few_kernel<unsigned char, T>), grid, block, 0, st, a, (const unsigned char *)nullptr, ldx);
     } else {
         with_type(xt, [&](auto *tag) {
             typedef std::remove_pointer_t<decltype(tag)> X;
-            hipLaunchKernelGGL((mx4_few_kernel<1, X, T>), grid, block, 0, st, a, (const X *)x, ldx);
+            hipLaunchKernelGGL((mx4_few_kernel<X, T>), grid, block, 0, st, a, (const X *)x, ldx);
         });
     }
 }
@@ -825,7 +834,7 @@ struct GradPlan {
 static GradPlan grad_plan(int I, int J, int C, bool weights)
 {
     GradPlan p = {};
-    p.cut = cut_product(I, J, std::max((C + 63) / 64, 1), 1, 8);
+    p.cut = cut_product(I, J, std::max((C + 63) / 64, 1), 1, 4, weights ? kWeightTiles : kInputTiles, 4);
     if (weights && p.cut.grid.parts > 1) p.db = round256((size_t)p.cut.grid.parts * (((size_t)I + 7) / 8 * 8) * 4);
     return p;
 }
@@ -836,13 +845,13 @@ static void grad_launch(const Cut &c, const GradArgs &a, hipStream_t st)
     const dim3 grid((unsigned)a.grid.per_xcd * kXCDs);
     // Loads to LDS ask for words, and reach 2^31 bytes from a tile's first row.
     const bool words = aligned_to(a.dy, 4) && a.ld % 2 == 0 && a.ld < ((size_t)1 << 22);
-    if (c.large) {
-        if (words) hipLaunchKernelGGL((gradient_kernel<4, 2, 2, 4, 2, WEIGHTS, true, T>), grid, dim3(512), 0, st, a);
-        else hipLaunchKernelGGL((gradient_kernel<4, 2, 2, 4, 2, WEIGHTS, false, T>), grid, dim3(512), 0, st, a);
-    } else {
-        if (words) hipLaunchKernelGGL((gradient_kernel<2, 2, 2, 2, 2, WEIGHTS, true, T>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((gradient_kernel<2, 2, 2, 2, 2, WEIGHTS, false, T>), grid, dim3(256), 0, st, a);
-    }
+#define LP_TILES(MB, NB, WM, WN)                                                                                                             \
+    hipLaunchKernelGGL((words ? gradient_kernel<MB, NB, WM, WN, WEIGHTS, true, T> : gradient_kernel<MB, NB, WM, WN, WEIGHTS, false, T>), grid, \
+                       dim3(WM * WN * 64), 0, st, a)
+    if (c.size == 0) LP_TILES(1, 2, 2, 2);
+    else if (c.size == 1) LP_TILES(2, 2, 2, 2);
+    else LP_TILES(4, 2, 2, 4);
+#undef LP_TILES
 }
 
 template <bool WEIGHTS>
@@ -923,7 +932,7 @@ extern "C" lp_status lp_mx4_fc_fwd(int M, int K, int Nout, const void *x_dev, lp
     const Sink out{y_dev, ldy, 0, bias_dev, act, 0};
     if (p.few) {
         a.out = out;
-        with_type(yt, [&](auto *tag) { few_launch<std::remove_pointer_t<decltype(tag)>>(p, a, x_dev, xt, ldx, st); });
+        with_type(yt, [&](auto *tag) { few_launch<std::remove_pointer_t<decltype(tag)>>(a, x_dev, xt, ldx, st); });
     } else if (a.grid.parts > 1) {
         float *sums = (float *)(work + p.codes + p.scales);
         const size_t part = (size_t)M * p.cut.ldp;
