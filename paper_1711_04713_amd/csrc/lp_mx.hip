@@ -10,6 +10,8 @@
 namespace lp {
 
 constexpr int kThreads = 256;
+// Counting launches: few blocks, so that the atomics of a counter (12 to 14 ns each, one after the other) hide behind the streaming.
+constexpr unsigned kCountThreads = 1024, kCountBlocks = 512;
 
 struct PieceGrid {
     unsigned rows, cols, per_row, magic, total; // pieces of eight per row (a multiple of 4) and in all
@@ -28,16 +30,22 @@ static bool piece_grid(size_t rows, size_t cols, size_t blocks, PieceGrid *g)
 
 static dim3 blocks_for(const PieceGrid &g) { return dim3((g.total + kThreads - 1) / kThreads); }
 
-// the draws of elements i .. i + 7
-__device__ __forceinline__ void draws8(uint64_t i, uint64_t seed, uint32_t (&w)[8])
+// the draws of elements i .. i + 7; whole: i is a multiple of 4 in every row
+__device__ __forceinline__ void draws8(uint64_t i, bool whole, uint64_t seed, uint32_t (&w)[8])
 {
-    if ((i & 3) == 0) {
+    if (whole) {
         const PhiloxBlock a = philox4x32_10(i >> 2, seed), b = philox4x32_10((i >> 2) + 1, seed);
 #pragma unroll
         for (int j = 0; j < 8; ++j) w[j] = j < 4 ? a.w[j & 3] : b.w[j & 3];
-    } else {
+    } else { // (three blocks: one a piece for each element took twice as long, 258 us for 117 M bfloat16 in rows of an odd length)
+        const PhiloxBlock a = philox4x32_10(i >> 2, seed), b = philox4x32_10((i >> 2) + 1, seed), c = philox4x32_10((i >> 2) + 2, seed);
+        const uint32_t all[12] = {a.w[0], a.w[1], a.w[2], a.w[3], b.w[0], b.w[1], b.w[2], b.w[3], c.w[0], c.w[1], c.w[2], c.w[3]};
+        const uint32_t one = 0u - ((uint32_t)i & 1), two = 0u - ((uint32_t)i >> 1 & 1);
+        uint32_t t[10];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = philox_draw(i + j, seed);
+        for (int j = 0; j < 10; ++j) t[j] = (all[j + 1] & one) | (all[j] & ~one);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = (t[j + 2] & two) | (t[j] & ~two);
     }
 }
 
@@ -61,12 +69,14 @@ __device__ __forceinline__ int mx4_code(float t, uint32_t draw)
 }
 
 template <typename T, int MODE, bool COUNT>
-__global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(const T *__restrict__ x, size_t ldx, PieceGrid g, unsigned *__restrict__ codes,
+__global__ __launch_bounds__(COUNT ? kCountThreads : kThreads) void mx4_quantize_kernel(const T *__restrict__ x, size_t ldx, PieceGrid g, unsigned *__restrict__ codes,
                                                                 unsigned char *__restrict__ scales, uint64_t seed,
                                                                 unsigned long long *zero_count, unsigned long long *sat_count)
 {
+    constexpr unsigned THREADS = COUNT ? kCountThreads : kThreads;
     unsigned zeros = 0, sats = 0;
-    for (unsigned p = blockIdx.x * kThreads + threadIdx.x; p < g.total; p += gridDim.x * kThreads) {
+#pragma unroll MODE == LP_ROUND_STOCHASTIC ? 1 : 2
+    for (unsigned p = blockIdx.x * THREADS + threadIdx.x; p < g.total; p += gridDim.x * THREADS) {
         unsigned row, piece;
         piece_place(p, g.per_row, g.magic, row, piece);
         const unsigned col = 8 * piece;
@@ -77,17 +87,16 @@ __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(const T *__restr
         if constexpr (MODE == LP_ROUND_NEAREST_EVEN) {
             w = mx4_word(v, e);
             if (COUNT) {
+                // (elements that do not exist are zeros)
+                zeros += n - __builtin_popcount(((w & 0x77777777u) + 0x77777777u) & 0x88888888u);
                 const float over = 7.0f * power_of_byte(e); // rounds to 8
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    zeros += j < n && (w >> (4 * j) & 7) == 0;
-                    sats += j < n && fabsf(v[j]) >= over;
-                }
+                for (int j = 0; j < 8; ++j) sats += fabsf(v[j]) >= over;
             }
         } else {
             const float inv = power_of_byte(254 - e);
             uint32_t draw[8] = {};
-            if constexpr (MODE == LP_ROUND_STOCHASTIC) draws8((uint64_t)row * g.cols + col, seed, draw);
+            if constexpr (MODE == LP_ROUND_STOCHASTIC) draws8((uint64_t)row * g.cols + col, (g.cols & 3) == 0, seed, draw);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float a = v[j] == v[j] ? v[j] : 0.0f;
@@ -107,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void mx4_quantize_kernel(const T *__restr
             zeros += __shfl_xor(zeros, d);
             sats += __shfl_xor(sats, d);
         }
-        add_block_counts<kThreads>(zeros, sats, zero_count, sat_count);
+        add_block_counts<THREADS>(zeros, sats, zero_count, sat_count);
     }
 }
 
@@ -138,7 +147,7 @@ __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const T *x, size_t
     const int e = min(max(block_exponent(v), 7), 254);
     const float inv = power_of_byte(260 - e);
     uint32_t draw[8] = {};
-    if constexpr (MODE == LP_ROUND_STOCHASTIC) draws8((uint64_t)row * g.cols + col, seed, draw);
+    if constexpr (MODE == LP_ROUND_STOCHASTIC) draws8((uint64_t)row * g.cols + col, (g.cols & 3) == 0, seed, draw);
     v2u w = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -272,8 +281,8 @@ extern "C" lp_status lp_mx4_quantize(const void *x_dev, lp_dtype xt, size_t rows
         typedef std::remove_pointer_t<decltype(tag)> T;
         with_mode(r, [&](auto mode) {
             constexpr int MODE = decltype(mode)::value;
-            const dim3 grid = count ? dim3(std::min(blocks_for(g).x, 512u)) : blocks_for(g);
-            hipLaunchKernelGGL((count ? mx4_quantize_kernel<T, MODE, true> : mx4_quantize_kernel<T, MODE, false>), grid, dim3(kThreads), 0, st,
+            const dim3 grid = count ? dim3(std::min((g.total + kCountThreads - 1) / kCountThreads, kCountBlocks)) : blocks_for(g);
+            hipLaunchKernelGGL((count ? mx4_quantize_kernel<T, MODE, true> : mx4_quantize_kernel<T, MODE, false>), grid, dim3(count ? kCountThreads : kThreads), 0, st,
                                (const T *)x_dev, ldx, g, (unsigned *)codes_dev, (unsigned char *)scales_dev, seed,
                                (unsigned long long *)zero_count_dev, (unsigned long long *)sat_count_dev);
         });
