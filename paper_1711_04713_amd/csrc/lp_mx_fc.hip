@@ -391,7 +391,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void mx4_few_kernel(const Mx4Arg
 //
 // A workgroup owns TI x TJ results, a wave MB x NB blocks of 32 x 32; a stage is 64 positions of the reduction in one of two
 // LDS buffers.  B's codes pass through registers, a block of 32 a thread, and are decoded one stage ahead; dY
-// comes by loads to LDS (or, where its rows do not start on words, through registers like the codes).  The matrix
+// comes by loads to LDS (or, where its rows do not start on words, through registers like the codes: 200 x 4096 from 1001
+// columns 13.6 us, from 1002 12.8; 8192 x 4096 from 14337 1020, from 14338 800).  The matrix
 // instruction wants eight neighbouring positions of a row or column in a lane: those of dY's rows lie together in memory
 // (16-byte piece p of row r at place p ^ (r % 8), as above); tiles with the reduction along their rows are read by
 // ds_read_b64_tr_b16, which hands each of 16 lanes four rows' elements of its column.  Their rows are 512 (or 256) bytes, so
@@ -500,7 +501,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     // dY.  The last stage of the whole reduction comes element by element through registers where it, or a row, ends inside a
     // piece: what lies behind must not be multiplied, not even by zero.
     const bool ragged = last == a.grid.stages && (last * 64 != a.C || (WEIGHTS && i0 + TI > a.I));
-    const int whole = WORDS ? last - ragged : first; // stages first .. whole - 1 come by loads to LDS
+    const int whole = last - ragged; // stages first .. whole - 1 come in whole pieces
     unsigned at[PER];
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
@@ -527,14 +528,19 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
             for (int q = decltype(from)::value; q < decltype(to)::value; ++q) load_lds16(rsrc, lds + buf * STAGE + (wave * PER + q) * 1024, at[q], 0);
         }
     };
-    v4u raw_dy[PER];
+    v4u raw_dy[PER] = {};
     auto fetch_dy = [&](int t) __attribute__((always_inline)) {
+        if (t >= whole) return;
+        typedef unsigned short V __attribute__((ext_vector_type(8), aligned(2)));
+        // (weights: a row's last piece reaches into the next row; the last row is not brought this way)
+        const size_t end = (size_t)(a.C - 1) * a.ld + a.I;
 #pragma unroll
         for (int q = 0; q < PER; ++q) {
             const int k = q * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
-            const int row = WEIGHTS ? t * 64 + r : i0 + r, col = WEIGHTS ? i0 + s * 8 : t * 64 + s * 8;
-            const int rows = WEIGHTS ? a.C : a.I, cols = WEIGHTS ? a.I : a.C;
-            raw_dy[q] = load_piece(a.dy + row * a.ld + col, row < rows && t < last ? cols - col : 0);
+            const int row = WEIGHTS ? t * 64 + r : min(i0 + r, a.I - 1), col = WEIGHTS ? i0 + s * 8 : t * 64 + s * 8;
+            const size_t from = row * a.ld + col;
+            if (WEIGHTS && a.ld < 8) raw_dy[q] = load_piece(a.dy + from, a.I - col);
+            else raw_dy[q] = __builtin_bit_cast(v4u, *reinterpret_cast<const V *>(a.dy + (WEIGHTS ? std::min(from, end - 8) : from)));
         }
     };
     // the same at once, a piece at a time
@@ -632,8 +638,9 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     // Stage t in buffer B: while it is multiplied the next one is completed in the other buffer.
     auto whole_stage = [&](int t, auto buffer) __attribute__((always_inline)) {
         constexpr int B = decltype(buffer)::value;
-        // loads that may still be on their way when the next stage's dY has arrived: the codes of the one behind it
-        constexpr int LATER = WORDS ? (WEIGHTS ? 3 : 2) : 0;
+        // loads that may still be on their way when the next stage's dY has arrived: the codes of the one behind it (all of them
+        // where dY is written to LDS from registers)
+        constexpr int LATER = WORDS ? (WEIGHTS ? 3 : 2) : 63;
         __builtin_amdgcn_sched_barrier(0);
         fragments(B, 1);
         load_dy(t + 1, B ^ 1, L1, L2);
@@ -649,7 +656,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
         }
         fragments(B, 3);
         LP_STEP(2)
-        if (WORDS && ragged && t + 2 == last) bring_dy(t + 1, B ^ 1);
+        if (ragged && t + 2 == last) bring_dy(t + 1, B ^ 1);
         arrived_but<LATER>();
         fragments(B ^ 1, 0);
         load_dy(t + 2, B, L0, L1);
