@@ -131,7 +131,16 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float *__restrict
     const int j = 8 * (int)piece;
     const float *q = parts + row * ldp + j; // (rows of the parts are whole pieces)
     v8f v = load8(q, 8);
-    for (int k = 1; k < count; ++k) v += load8(q + k * part, 8);
+    int k = 1;
+    for (; k + 8 <= count; k += 8) { // eight on their way at a time
+        v8f w[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) w[u] = load8(q + (k + u) * part, 8);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v += w[u];
+    }
+#pragma unroll 4
+    for (; k < count; ++k) v += load8(q + k * part, 8);
     put8(out, (T *)out.y + row * out.ld + j, out.bias + j, J - j, v);
 }
 
@@ -712,11 +721,12 @@ struct TileCost {
     int i, j;
     double alone, full, ends, more;
 };
-// 64 x 64, 128 x 128 (four buffers each), 256 x 256 (two); a stage is 256 positions
-constexpr TileCost kMx4Tiles[3] = {{64, 64, 0.215, 0.255, 0.7, 0.7}, {128, 128, 0.43, 0.645, 1.5, 0.3}, {256, 256, 1.25, 2.0, 1.5, 0.9}};
+// 64 x 64, 128 x 128 (four buffers each), 256 x 256 (two), 128 x 128 with two, which lets two workgroups of a unit work and end
+// side by side; a stage is 256 positions
+constexpr TileCost kMx4Tiles[4] = {{64, 64, 0.23, 0.215, 1.85, 0.85}, {128, 128, 0.43, 0.555, 3.3, 2.9}, {256, 256, 1.3, 1.67, 4.8, 2.0}, {128, 128, 0.62, 0.525, 2.55, 1.3}};
 // 64 x 128, 128 x 128, 256 x 256; a stage is 64 positions
-constexpr TileCost kInputTiles[3] = {{64, 128, 0.46, 0.38, 2.5, 0.25}, {128, 128, 0.56, 0.535, 3.0, 0.6}, {256, 256, 1.2, 1.75, 3.3, 2.0}};
-constexpr TileCost kWeightTiles[3] = {{64, 128, 0.48, 0.43, 2.5, 0.25}, {128, 128, 0.57, 0.645, 3.0, 0.6}, {256, 256, 1.65, 2.2, 3.3, 2.0}};
+constexpr TileCost kInputTiles[3] = {{64, 128, 0.39, 0.315, 2.65, 0.45}, {128, 128, 0.505, 0.455, 3.15, 0.0}, {256, 256, 1.19, 1.34, 4.1, 0.0}};
+constexpr TileCost kWeightTiles[3] = {{64, 128, 0.91, 0.405, 4.75, 0.65}, {128, 128, 0.77, 0.535, 4.95, 1.75}, {256, 256, 1.265, 1.51, 8.5, 6.1}};
 
 // How a product I x J with `stages` stages of its reduction is cut into workgroups.
 struct Cut {
@@ -726,14 +736,15 @@ struct Cut {
     double us;
 };
 
-// The cheapest of the tiles and numbers of parts, by an estimate that the tables above were fitted to (1322 timings of 162
-// problems: the choice costs 1.2 % on the average and 20 % at most).  Results leave at 16 GB/s a compute unit; joining the
-// parts is a launch, and their sums go through memory at 6 TB/s.  A part has `step` stages or a multiple of them, and `least`
-// at least.
-static Cut cut_product(int I, int J, int stages, int step, int least, const TileCost (&tiles)[3], int out_bytes)
+// The cheapest of the tiles and numbers of parts, by an estimate that the tables above were fitted to (1864 timings of 232
+// problems: the choice costs 0.6 % on the average; it is a part too many or too few, 10 to 30 % of 5 to 15 us, where it is
+// worst).  Results leave at 44 GB/s a compute unit; joining the parts is a launch, and their sums go through memory at
+// 7.5 TB/s.  A part has `step` stages or a multiple of them, and `least` at least.
+template <int SIZES>
+static Cut cut_product(int I, int J, int stages, int step, int least, const TileCost (&tiles)[SIZES], int out_bytes)
 {
     Cut best = {};
-    for (int size = 0; size < 3; ++size) {
+    for (int size = 0; size < SIZES; ++size) {
         const TileCost &c = tiles[size];
         const long long ti = (I + c.i - 1) / c.i, tj = (J + c.j - 1) / c.j;
         for (int parts = 1; parts <= 32; parts += parts < 4 ? 1 : parts / 2) { // 1 2 3 4 6 9 13 19 28
@@ -742,9 +753,9 @@ static Cut cut_product(int I, int J, int stages, int step, int least, const Tile
             const long long work = ti * tj * real;
             const double rounds = (double)((work + kCUs - 1) / kCUs), busy = std::min(1.0, (double)work / kCUs);
             const double stage = rounds > 1 ? std::max(c.alone, rounds * c.full) : c.alone + std::max(0.0, c.full - c.alone) * busy;
-            const double out = (double)c.i * c.j * (real > 1 ? 4 : out_bytes) / 16384.0 * busy;
+            const double out = (double)c.i * c.j * (real > 1 ? 4 : out_bytes) / 45056.0 * busy;
             double us = 2.5 + c.ends + std::min(each, stages) * stage + (rounds - 1) * c.more + rounds * out;
-            if (real > 1) us += 2.3 + (double)real * I * J * 8 / 6e6;
+            if (real > 1) us += 2.3 + (double)real * I * J * 8 / 7.5e6;
             if (best.us == 0 || us < best.us) {
                 best.us = us;
                 best.size = size;
@@ -814,7 +825,8 @@ static void mx4_launch(const Cut &c, const Mx4Args &a, hipStream_t st)
     const dim3 grid((unsigned)a.grid.per_xcd * kXCDs);
     if (c.size == 0) hipLaunchKernelGGL((mx4_product_kernel<1, 1, 2, 2, 4, T>), grid, dim3(256), 0, st, a);
     else if (c.size == 1) hipLaunchKernelGGL((mx4_product_kernel<2, 2, 2, 2, 4, T>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((mx4_product_kernel<4, 2, 2, 4, 2, T>), grid, dim3(512), 0, st, a);
+    else if (c.size == 2) hipLaunchKernelGGL((mx4_product_kernel<4, 2, 2, 4, 2, T>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((mx4_product_kernel<2, 2, 2, 2, 2, T>), grid, dim3(256), 0, st, a);
 }
 
 template <typename T>
