@@ -40,13 +40,13 @@ __device__ __forceinline__ void all_arrived() { arrived_but<0>(); }
 
 // -------------------------------------------------------------------------------- results
 
-// Where a product's sums go: out[i][j] = act(sum + bias[j]), rounded once.  A product that is cut along its reduction
-// writes 32-bit sums of its parts to the workspace in the same way (no bias, no function), part p `part` elements further.
-// accumulate: what is there is added before the rounding.
+// Where a product's sums go: out[i][j] = act(sum + bias[j]), rounded once.  accumulate: what is there is added before the
+// rounding.  (db, weights only, may be null: the sums of dY, one for each row of out.)
 struct Sink {
     void *y;
-    size_t ld, part;
+    size_t ld;
     const float *bias;
+    float *db;
     lp_actfn act;
     int accumulate;
 };
@@ -60,17 +60,16 @@ __device__ __forceinline__ void put8(const Sink &s, T *to, const float *bias, in
     store8(to, n, act_values(v, s.act));
 }
 
-// A wave's results, MB x NB blocks of 32 rows x 32 columns from (i0, j0) on: 32 rows at a time through a piece of LDS of its
-// own, so that they leave as whole rows, eight neighbours a lane.  In the accumulators a lane holds, of row lane % 32 of a
-// block, columns 8 g + 4 (lane / 32) + 0..3 in registers 4 g ..
+// A wave's results, MB x NB blocks of 32 rows x 32 columns from (i0, j0) of a tile on, of which I x J exist: 32 rows at a time
+// through a piece of LDS of its own, so that they leave as whole rows, eight neighbours a lane.  In the accumulators a lane
+// holds, of row lane % 32 of a block, columns 8 g + 4 (lane / 32) + 0..3 in registers 4 g ..
 constexpr int result_row(int NB) { return NB * 32 + 4; } // floats, padded
 constexpr int result_bytes(int NB) { return 32 * result_row(NB) * 4; }
-template <int MB, int NB, typename T>
-__device__ __forceinline__ void put_results(const Sink &out, int part, float *mine, const v16f (&acc)[NB][MB], int i0, int j0, int I, int J)
+template <int MB, int NB, typename PUT>
+__device__ __forceinline__ void put_blocks(float *mine, const v16f (&acc)[NB][MB], int i0, int j0, int I, int J, PUT put)
 {
     constexpr int ROW = result_row(NB);
     const int lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
-    T *y = (T *)out.y + part * out.part;
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
         const int ib = i0 + b * 32;
@@ -88,60 +87,108 @@ __device__ __forceinline__ void put_results(const Sink &out, int part, float *mi
             const int k = q * 64 + lane, row = k / (NB * 4), col = k % (NB * 4) * 8;
             const v4f lo = *(const v4f *)(mine + row * ROW + col), hi = *(const v4f *)(mine + row * ROW + col + 4);
             const int i = ib + row, j = j0 + col;
-            if (i < I && j < J) put8(out, y + i * out.ld + j, out.bias + j, J - j, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            if (i < I && j < J) put(i, j, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 }
 
-// Which tile a workgroup computes: consecutive workgroups go round the dies, each die has a run of consecutive items; an item
-// is a part of the reduction and a tile, row tiles walked kTileGroup at a time: 32 workgroups of a die share 4 x 8 tiles.
+// Which tile a workgroup computes, and which stages of the reduction.  The first `whole` tiles, a multiple of the compute
+// units, are one workgroup each and go straight to the results; every one of the rest is cut along the reduction into `parts`,
+// whose 32-bit sums meet in the workspace (one part: straight to the results too).  A last round that fills a few of the
+// units, and a product that has few tiles, are spread over all of them this way.
+//
+// Consecutive workgroups go round the dies, each die has a run of consecutive tiles, row tiles walked kTileGroup at a time: 32
+// workgroups of a die share 4 x 8 tiles.
 constexpr int kTileGroup = 4;
 struct Grid {
-    int tiles_i, tiles_j, stages, stages_per_part, parts, work, per_xcd;
+    int tiles_i, tiles_j, stages, whole, rest, parts, stages_per_part, work, per_xcd; // work = rest * parts
+    float *sums;                                                                      // TI * TJ of each part and tile, then TI of dY
 };
 struct Place {
-    int part, tile_i, tile_j, first, last; // stages first .. last - 1
+    int tile_i, tile_j, first, last; // stages first .. last - 1
+    int sums;                        // number of the part and tile, or -1
 };
-__device__ __forceinline__ bool find_place(const Grid &g, Place *p)
+__device__ __forceinline__ void place_tile(const Grid &g, int tile, Place *p)
 {
-    const int item = (blockIdx.x % kXCDs) * g.per_xcd + blockIdx.x / kXCDs;
-    if (item >= g.work) return false;
     // (divisions run on the vector unit: what comes back is said to be the same in all lanes)
-    const int tiles = g.tiles_i * g.tiles_j;
-    p->part = __builtin_amdgcn_readfirstlane(item / tiles);
-    const int tile = item - p->part * tiles, group = __builtin_amdgcn_readfirstlane(tile / (kTileGroup * g.tiles_j));
+    const int group = __builtin_amdgcn_readfirstlane(tile / (kTileGroup * g.tiles_j));
     const int in_group = tile - group * kTileGroup * g.tiles_j, rows = min(kTileGroup, g.tiles_i - group * kTileGroup);
     p->tile_j = __builtin_amdgcn_readfirstlane(in_group / rows);
     p->tile_i = group * kTileGroup + in_group - p->tile_j * rows;
-    p->first = p->part * g.stages_per_part;
+}
+__device__ __forceinline__ bool find_place(const Grid &g, Place *p)
+{
+    const bool whole = (int)blockIdx.x < g.whole;
+    const int b = blockIdx.x - (whole ? 0 : g.whole), item = (b % kXCDs) * (whole ? g.whole / kXCDs : g.per_xcd) + b / kXCDs;
+    if (whole) {
+        place_tile(g, item, p);
+        p->first = 0;
+        p->last = g.stages;
+        p->sums = -1;
+        return true;
+    }
+    if (item >= g.work) return false;
+    const int part = __builtin_amdgcn_readfirstlane(item / g.rest);
+    place_tile(g, g.whole + item - part * g.rest, p);
+    p->first = part * g.stages_per_part;
     p->last = min(g.stages, p->first + g.stages_per_part);
+    p->sums = g.parts > 1 ? item : -1;
     return true;
 }
+constexpr size_t tile_sums(int TI, int TJ) { return (size_t)TI * TJ + TI; } // floats
 
-// y = act(sum of the parts + bias): a thread takes eight neighbours of a row
-template <typename T>
-__global__ __launch_bounds__(256) void join_parts_kernel(const float *__restrict__ parts, int count, size_t part, size_t ldp, Sink out, int J, unsigned per_row,
-                                                         unsigned magic, unsigned total)
+template <int TI, int TJ, int MB, int NB, typename OutT>
+__device__ __forceinline__ void put_results(const Grid &g, const Sink &out, const Place &p, float *mine, const v16f (&acc)[NB][MB], int i0, int j0, int I, int J)
 {
-    const unsigned p = blockIdx.x * 256 + threadIdx.x;
-    if (p >= total) return;
-    unsigned row, piece;
-    piece_place(p, per_row, magic, row, piece);
-    const int j = 8 * (int)piece;
-    const float *q = parts + row * ldp + j; // (rows of the parts are whole pieces)
-    v8f v = load8(q, 8);
-    int k = 1;
-    for (; k + 8 <= count; k += 8) { // eight on their way at a time
-        v8f w[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) w[u] = load8(q + (k + u) * part, 8);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) v += w[u];
+    const int ti = p.tile_i * TI, tj = p.tile_j * TJ;
+    if (p.sums >= 0) {
+        float *to = g.sums + p.sums * tile_sums(TI, TJ);
+        put_blocks<MB, NB>(mine, acc, i0, j0, I - ti, J - tj, [&](int i, int j, v8f v) __attribute__((always_inline)) {
+            *(v4f *)(to + i * TJ + j) = __builtin_shufflevector(v, v, 0, 1, 2, 3); // (whole pieces, where the row ends inside too)
+            *(v4f *)(to + i * TJ + j + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+        });
+    } else {
+        OutT *to = (OutT *)out.y + ti * out.ld + tj;
+        const float *bias = out.bias + tj;
+        put_blocks<MB, NB>(mine, acc, i0, j0, I - ti, J - tj, [&](int i, int j, v8f v) __attribute__((always_inline)) {
+            put8(out, to + i * out.ld + j, bias + j, J - tj - j, v);
+        });
     }
+}
+
+// y = act(sum of the parts + bias), db the same of the rows' sums: a thread takes eight neighbours of a row of a tile
+template <typename T>
+__global__ __launch_bounds__(256) void join_parts_kernel(const Grid g, Sink out, int TI, int TJ, int I, int J, int per_tile)
+{
+    const int rest = blockIdx.x / per_tile, within = blockIdx.x - rest * per_tile;
+    Place p;
+    place_tile(g, g.whole + rest, &p);
+    const size_t tile = (size_t)TI * TJ + TI, part = tile * g.rest;
+    const float *sums = g.sums + rest * tile;
+    auto joined = [&](const float *q, auto load) __attribute__((always_inline)) {
+        auto v = load(q);
+        int k = 1;
+        for (; k + 8 <= g.parts; k += 8) { // eight on their way at a time
+            decltype(v) w[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) w[u] = load(q + (k + u) * part);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v += w[u];
+        }
 #pragma unroll 4
-    for (; k < count; ++k) v += load8(q + k * part, 8);
-    put8(out, (T *)out.y + row * out.ld + j, out.bias + j, J - j, v);
+        for (; k < g.parts; ++k) v += load(q + k * part);
+        return v;
+    };
+    const int piece = within * 256 + threadIdx.x, row = piece / (TJ / 8), col = piece % (TJ / 8) * 8;
+    const int i = p.tile_i * TI + row, j = p.tile_j * TJ + col;
+    if (row < TI && i < I && j < J)
+        put8(out, (T *)out.y + i * out.ld + j, out.bias + j, J - j, joined(sums + row * TJ + col, [](const float *q) { return load8(q, 8); }));
+    const int r = p.tile_i * TI + threadIdx.x;
+    if (out.db && p.tile_j == 0 && within == 0 && threadIdx.x < TI && r < I) {
+        const float v = joined(sums + TI * TJ + threadIdx.x, [](const float *q) { return *q; });
+        out.db[r] = out.accumulate ? out.db[r] + v : v;
+    }
 }
 
 // ------------------------------------------------------------------------------- mx4 times mx4
@@ -312,7 +359,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
         if (t + 4 >= last) break;
     }
     all_arrived();
-    put_results<MB, NB, OutT>(a.out, p.part, (float *)(lds + wave * result_bytes(NB)), acc, m0 + wm * MB * 32, n0 + wn * NB * 32, a.M, a.N);
+    put_results<TM, TN, MB, NB, OutT>(a.grid, a.out, p, (float *)(lds + wave * result_bytes(NB)), acc, wm * MB * 32, wn * NB * 32, a.M, a.N);
 }
 
 // Few rows (16 at most): the weights are all that matters, and every byte of them is read once, straight into the registers that the matrix
@@ -415,9 +462,6 @@ struct GradArgs {
     const unsigned char *codes, *scales;
     int I, J, C, blocks; // blocks of 32 in a row of B
     Grid grid;
-    float *db;           // sums of dY over the reduction (weights only; may be null), part p at db + p * db_part
-    size_t db_part;
-    int db_accumulate;
     Sink out;
 };
 
@@ -614,7 +658,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
         for (int b = 0; b < NB; ++b) fb[s & 1][b] = tr_read(buf * STAGE + bpos[b] + s * 16 * BROW, BROW);
     };
     // sums of dY: a lane's eight positions of its column of each block
-    const bool sum_dy = WEIGHTS && a.db && p.tile_j == 0 && wn == 0;
+    const bool sum_dy = WEIGHTS && a.out.db && p.tile_j == 0 && wn == 0;
     float db[MB] = {};
     auto add_dy = [&](int s) __attribute__((always_inline)) {
         if constexpr (WEIGHTS) {
@@ -692,12 +736,13 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
 #pragma unroll
         for (int b = 0; b < MB; ++b) {
             const float v = db[b] + __shfl_xor(db[b], 32);
-            const int i = i0 + (wm * MB + b) * 32 + l32;
-            float *to = a.db + p.part * a.db_part + i;
-            if (h == 0 && i < a.I) *to = a.db_accumulate ? *to + v : v;
+            const int i = (wm * MB + b) * 32 + l32;
+            if (h != 0 || i0 + i >= a.I) continue;
+            if (p.sums >= 0) a.grid.sums[p.sums * tile_sums(TI, TJ) + TI * TJ + i] = v;
+            else a.out.db[i0 + i] = a.out.accumulate ? a.out.db[i0 + i] + v : v;
         }
     }
-    put_results<MB, NB, OutT>(a.out, p.part, (float *)(lds + wave * result_bytes(NB)), acc, i0 + wm * MB * 32, j0 + wn * NB * 32, a.I, a.J);
+    put_results<TI, TJ, MB, NB, OutT>(a.grid, a.out, p, (float *)(lds + wave * result_bytes(NB)), acc, wm * MB * 32, wn * NB * 32, a.I, a.J);
 }
 
 // ------------------------------------------------------------------------------------- plans
@@ -721,6 +766,12 @@ struct TileCost {
     int i, j;
     double alone, full, ends, more;
 };
+// A stage of each of `work` workgroups.
+static double stage_cost(const TileCost &c, long long work)
+{
+    const double last = work % kCUs ? std::min(c.alone, c.full) + std::max(0.0, c.full - c.alone) * (work % kCUs) / kCUs : 0.0;
+    return std::max(c.alone, (double)(work / kCUs) * c.full + last);
+}
 // 64 x 64, 128 x 128 (four buffers each), 256 x 256 (two), 128 x 128 with two, which lets two workgroups of a unit work and end
 // side by side; a stage is 256 positions
 constexpr TileCost kMx4Tiles[4] = {{64, 64, 0.23, 0.215, 1.85, 0.85}, {128, 128, 0.43, 0.555, 3.3, 2.9}, {256, 256, 1.3, 1.67, 4.8, 2.0}, {128, 128, 0.62, 0.525, 2.55, 1.3}};
@@ -730,14 +781,14 @@ constexpr TileCost kWeightTiles[3] = {{64, 128, 0.91, 0.405, 4.75, 0.65}, {128, 
 
 // How a product I x J with `stages` stages of its reduction is cut into workgroups.
 struct Cut {
-    int size; // which of the tiles
+    int size, i, j; // which of the tiles
     Grid grid;
-    size_t ldp, sums; // the parts' sums: row length, bytes (0: one part)
+    size_t sums;    // bytes (0: one part)
     double us;
 };
 
-// The cheapest of the tiles and numbers of parts, by an estimate that the tables above were fitted to (1864 timings of 232
-// problems: the choice costs 0.6 % on the average; it is a part too many or too few, 10 to 30 % of 5 to 15 us, where it is
+// The cheapest of the tiles and numbers of parts, by an estimate that the tables above were fitted to (2102 timings of 268
+// problems: the choice costs 0.7 % on the average; it is a part too many or too few, 10 to 30 % of 5 to 15 us, where it is
 // worst).  Results leave at 44 GB/s a compute unit; joining the parts is a launch, and their sums go through memory at
 // 7.5 TB/s.  A part has `step` stages or a multiple of them, and `least` at least.
 template <int SIZES>
@@ -746,28 +797,35 @@ static Cut cut_product(int I, int J, int stages, int step, int least, const Tile
     Cut best = {};
     for (int size = 0; size < SIZES; ++size) {
         const TileCost &c = tiles[size];
-        const long long ti = (I + c.i - 1) / c.i, tj = (J + c.j - 1) / c.j;
-        for (int parts = 1; parts <= 32; parts += parts < 4 ? 1 : parts / 2) { // 1 2 3 4 6 9 13 19 28
-            if (parts > 1 && (stages < parts * least || ti * tj * parts > 4 * kCUs)) break;
-            const int each = ((stages + parts - 1) / parts + step - 1) / step * step, real = (stages + each - 1) / each;
-            const long long work = ti * tj * real;
-            const double rounds = (double)((work + kCUs - 1) / kCUs), busy = std::min(1.0, (double)work / kCUs);
-            const double stage = rounds > 1 ? std::max(c.alone, rounds * c.full) : c.alone + std::max(0.0, c.full - c.alone) * busy;
-            const double out = (double)c.i * c.j * (real > 1 ? 4 : out_bytes) / 45056.0 * busy;
-            double us = 2.5 + c.ends + std::min(each, stages) * stage + (rounds - 1) * c.more + rounds * out;
-            if (real > 1) us += 2.3 + (double)real * I * J * 8 / 7.5e6;
-            if (best.us == 0 || us < best.us) {
-                best.us = us;
-                best.size = size;
-                best.grid = Grid{(int)ti, (int)tj, stages, each, real, (int)std::min<long long>(work, 0x7fffffff), 0};
+        const long long ti = (I + c.i - 1) / c.i, tj = (J + c.j - 1) / c.j, all = ti * tj;
+        // all tiles in parts, or those of the last round only
+        for (int keep = 0; keep < (all > kCUs && all % kCUs ? 2 : 1); ++keep) {
+            const long long full = keep ? all / kCUs : 0, rest = all - full * kCUs;
+            for (int parts = 1 + keep; parts <= 32; parts += parts < 4 ? 1 : parts / 2) { // 1 2 3 4 6 9 13 19 28
+                if (parts > 1 && (stages < parts * least || rest * parts > 4 * kCUs)) break;
+                const int each = ((stages + parts - 1) / parts + step - 1) / step * step, real = (stages + each - 1) / each;
+                if (keep && real == 1) continue;
+                const long long work = rest * real, rounds = (work + kCUs - 1) / kCUs;
+                const double ends = 2.5 + c.ends + (full + rounds - 1) * c.more, out = (double)c.i * c.j / 45056.0;
+                const double leave = full * out * out_bytes + rounds * out * std::min(1.0, (double)work / kCUs) * (real > 1 ? 4 : out_bytes);
+                double us = ends + leave + full * stages * c.full + std::min(each, stages) * (stage_cost(c, full * kCUs + work) - full * c.full);
+                if (real > 1) us += 2.3 + (double)real * (keep ? (double)rest * c.i * c.j : (double)I * J) * 8 / 7.5e6;
+                if (best.us == 0 || us < best.us) {
+                    best.us = us;
+                    best.size = size;
+                    best.i = c.i;
+                    best.j = c.j;
+                    best.grid = Grid{(int)ti, (int)tj, stages, (int)full * kCUs, (int)rest, real, each, (int)work, (int)((work + kXCDs - 1) / kXCDs), nullptr};
+                }
             }
         }
     }
-    best.grid.per_xcd = (best.grid.work + kXCDs - 1) / kXCDs;
-    best.ldp = ((size_t)J + 7) / 8 * 8;
-    best.sums = best.grid.parts > 1 ? round256((size_t)best.grid.parts * I * best.ldp * 4) : 0;
+    const Grid &g = best.grid;
+    best.sums = g.parts > 1 ? round256(g.work * tile_sums(best.i, best.j) * 4) : 0;
     return best;
 }
+
+static unsigned workgroups(const Grid &g) { return (unsigned)g.whole + (unsigned)g.per_xcd * kXCDs; }
 
 // f(type tag) for the element type of t
 template <typename F>
@@ -779,12 +837,12 @@ static void with_type(lp_dtype t, F f)
 }
 
 // out = act(sum of the parts + bias)
-static void join_parts(const float *sums, int parts, size_t part, size_t ldp, lp_dtype t, const Sink &out, int I, int J, hipStream_t st)
+static void join_parts(const Cut &c, const Grid &g, lp_dtype t, const Sink &out, int I, int J, hipStream_t st)
 {
-    const unsigned per_row = (unsigned)(ldp / 8), total = per_row * (unsigned)I;
+    const int per_tile = (std::min(c.i, I) * (c.j / 8) + 255) / 256;
     with_type(t, [&](auto *tag) {
         typedef std::remove_pointer_t<decltype(tag)> T;
-        hipLaunchKernelGGL(join_parts_kernel<T>, dim3((total + 255) / 256), dim3(256), 0, st, sums, parts, part, ldp, out, J, per_row, piece_magic(per_row), total);
+        hipLaunchKernelGGL(join_parts_kernel<T>, dim3((unsigned)g.rest * per_tile), dim3(256), 0, st, g, out, c.i, c.j, I, J, per_tile);
     });
 }
 
@@ -822,7 +880,7 @@ static Mx4Plan mx4_plan(int M, int K, int Nout)
 template <typename T>
 static void mx4_launch(const Cut &c, const Mx4Args &a, hipStream_t st)
 {
-    const dim3 grid((unsigned)a.grid.per_xcd * kXCDs);
+    const dim3 grid(workgroups(a.grid));
     if (c.size == 0) hipLaunchKernelGGL((mx4_product_kernel<1, 1, 2, 2, 4, T>), grid, dim3(256), 0, st, a);
     else if (c.size == 1) hipLaunchKernelGGL((mx4_product_kernel<2, 2, 2, 2, 4, T>), grid, dim3(256), 0, st, a);
     else if (c.size == 2) hipLaunchKernelGGL((mx4_product_kernel<4, 2, 2, 4, 2, T>), grid, dim3(512), 0, st, a);
@@ -843,25 +901,15 @@ static void few_launch(const Mx4Args &a, const void *x, lp_dtype xt, size_t ldx,
     }
 }
 
-// Gradients: workspace of the parts' sums, then of the bias's.
-struct GradPlan {
-    Cut cut;
-    size_t db;
-    size_t total() const { return cut.sums + db; }
-};
-
-static GradPlan grad_plan(int I, int J, int C, bool weights)
+static Cut grad_cut(int I, int J, int C, bool weights)
 {
-    GradPlan p = {};
-    p.cut = cut_product(I, J, std::max((C + 63) / 64, 1), 1, 4, weights ? kWeightTiles : kInputTiles, 4);
-    if (weights && p.cut.grid.parts > 1) p.db = round256((size_t)p.cut.grid.parts * (((size_t)I + 7) / 8 * 8) * 4);
-    return p;
+    return cut_product(I, J, std::max((C + 63) / 64, 1), 1, 4, weights ? kWeightTiles : kInputTiles, 4);
 }
 
 template <bool WEIGHTS, typename T>
 static void grad_launch(const Cut &c, const GradArgs &a, hipStream_t st)
 {
-    const dim3 grid((unsigned)a.grid.per_xcd * kXCDs);
+    const dim3 grid(workgroups(a.grid));
     // Loads to LDS ask for words, and reach 2^31 bytes from a tile's first row.
     const bool words = aligned_to(a.dy, 4) && a.ld % 2 == 0 && a.ld < ((size_t)1 << 22);
 #define LP_TILES(MB, NB, WM, WN)                                                                                                             \
@@ -874,28 +922,14 @@ static void grad_launch(const Cut &c, const GradArgs &a, hipStream_t st)
 }
 
 template <bool WEIGHTS>
-static void gradient(const GradPlan &p, GradArgs a, lp_dtype t, const Sink &out, float *dbias, unsigned char *work, hipStream_t st)
+static void gradient(const Cut &c, GradArgs a, lp_dtype t, const Sink &out, void *work, hipStream_t st)
 {
-    a.grid = p.cut.grid;
-    a.db = dbias;
-    a.db_accumulate = out.accumulate;
-    if (p.cut.grid.parts > 1) {
-        float *sums = (float *)work, *db = (float *)(work + p.cut.sums);
-        const size_t part = (size_t)a.I * p.cut.ldp, db_part = ((size_t)a.I + 7) / 8 * 8;
-        a.out = Sink{sums, p.cut.ldp, part, nullptr, LP_ACT_NONE, 0};
-        if (dbias) {
-            a.db = db;
-            a.db_part = db_part;
-            a.db_accumulate = 0;
-        }
-        grad_launch<WEIGHTS, float>(p.cut, a, st);
-        join_parts(sums, a.grid.parts, part, p.cut.ldp, t, out, a.I, a.J, st);
-        if (dbias) join_parts(db, a.grid.parts, db_part, db_part, LP_F32, Sink{dbias, 0, 0, nullptr, LP_ACT_NONE, out.accumulate}, 1, a.I, st);
-    } else {
-        a.out = out;
-        if (t == LP_F32) grad_launch<WEIGHTS, float>(p.cut, a, st);
-        else grad_launch<WEIGHTS, __bf16>(p.cut, a, st);
-    }
+    a.grid = c.grid;
+    a.grid.sums = (float *)work;
+    a.out = out;
+    if (t == LP_F32) grad_launch<WEIGHTS, float>(c, a, st);
+    else grad_launch<WEIGHTS, __bf16>(c, a, st);
+    if (a.grid.parts > 1) join_parts(c, a.grid, t, out, a.I, a.J, st);
 }
 
 } // namespace lp
@@ -948,20 +982,14 @@ extern "C" lp_status lp_mx4_fc_fwd(int M, int K, int Nout, const void *x_dev, lp
         a.xc = work;
         a.xs = work + p.codes;
     }
-    const Sink out{y_dev, ldy, 0, bias_dev, act, 0};
-    if (p.few) {
-        a.out = out;
-        with_type(yt, [&](auto *tag) { few_launch<std::remove_pointer_t<decltype(tag)>>(a, x_dev, xt, ldx, st); });
-    } else if (a.grid.parts > 1) {
-        float *sums = (float *)(work + p.codes + p.scales);
-        const size_t part = (size_t)M * p.cut.ldp;
-        a.out = Sink{sums, p.cut.ldp, part, nullptr, LP_ACT_NONE, 0};
-        mx4_launch<float>(p.cut, a, st);
-        join_parts(sums, a.grid.parts, part, p.cut.ldp, yt, out, M, Nout, st);
-    } else {
-        a.out = out;
-        with_type(yt, [&](auto *tag) { mx4_launch<std::remove_pointer_t<decltype(tag)>>(p.cut, a, st); });
-    }
+    a.grid.sums = (float *)(work + p.codes + p.scales);
+    a.out = Sink{y_dev, ldy, bias_dev, nullptr, act, 0};
+    with_type(yt, [&](auto *tag) {
+        typedef std::remove_pointer_t<decltype(tag)> T;
+        if (p.few) few_launch<T>(a, x_dev, xt, ldx, st);
+        else mx4_launch<T>(p.cut, a, st);
+    });
+    if (a.grid.parts > 1) join_parts(p.cut, a.grid, yt, a.out, M, Nout, st);
     return launch_status();
 }
 
@@ -969,7 +997,7 @@ extern "C" lp_status lp_mx4_fc_dgrad_workspace_bytes(int M, int K, int Nout, siz
 {
     if (!bytes_host || !sizes_ok(M, K, Nout)) return LP_EINVAL;
     if (!sizes_taken(M, K, Nout)) return LP_EUNSUPPORTED;
-    *bytes_host = M ? grad_plan(M, K, Nout, false).total() : 0;
+    *bytes_host = M ? grad_cut(M, K, Nout, false).sums : 0;
     return LP_OK;
 }
 
@@ -981,8 +1009,8 @@ extern "C" lp_status lp_mx4_fc_dgrad(int M, int K, int Nout, const void *dy_dev,
     if (!sizes_taken(M, K, Nout) || dxt == LP_F16) return LP_EUNSUPPORTED;
     if (M == 0) return LP_OK;
     if (!floats_ok(dy_dev, LP_BF16, (size_t)Nout, lddy) || !mx4_ok(w_codes_dev, w_scales_dev) || !floats_ok(dx_dev, dxt, (size_t)K, lddx)) return LP_EINVAL;
-    const GradPlan p = grad_plan(M, K, Nout, false);
-    if (const lp_status s = workspace_status(p.total(), workspace_dev, workspace_bytes)) return s;
+    const Cut c = grad_cut(M, K, Nout, false);
+    if (const lp_status s = workspace_status(c.sums, workspace_dev, workspace_bytes)) return s;
     clear_stale_error();
     GradArgs a = {};
     a.dy = (const __bf16 *)dy_dev;
@@ -993,7 +1021,7 @@ extern "C" lp_status lp_mx4_fc_dgrad(int M, int K, int Nout, const void *dy_dev,
     a.J = K;
     a.C = Nout;
     a.blocks = (int)mx4_blocks((size_t)K);
-    gradient<false>(p, a, dxt, Sink{dx_dev, lddx, 0, nullptr, LP_ACT_NONE, 0}, nullptr, (unsigned char *)workspace_dev, as_stream(stream));
+    gradient<false>(c, a, dxt, Sink{dx_dev, lddx, nullptr, nullptr, LP_ACT_NONE, 0}, workspace_dev, as_stream(stream));
     return launch_status();
 }
 
@@ -1001,7 +1029,7 @@ extern "C" lp_status lp_ckpt8_fc_wgrad_workspace_bytes(int M, int K, int Nout, s
 {
     if (!bytes_host || !sizes_ok(M, K, Nout)) return LP_EINVAL;
     if (!sizes_taken(M, K, Nout)) return LP_EUNSUPPORTED;
-    *bytes_host = grad_plan(Nout, K, M, true).total();
+    *bytes_host = grad_cut(Nout, K, M, true).sums;
     return LP_OK;
 }
 
@@ -1013,8 +1041,8 @@ extern "C" lp_status lp_ckpt8_fc_wgrad(int M, int K, int Nout, const void *dy_de
     if (!sizes_taken(M, K, Nout) || dwt == LP_F16) return LP_EUNSUPPORTED;
     if (M && (!floats_ok(dy_dev, LP_BF16, (size_t)Nout, lddy) || !x_codes_dev || !aligned16(x_codes_dev) || !x_scales_dev)) return LP_EINVAL;
     if (!floats_ok(dw_dev, dwt, (size_t)K, lddw) || !aligned_to(dbias_dev, 4)) return LP_EINVAL;
-    const GradPlan p = grad_plan(Nout, K, M, true);
-    if (const lp_status s = workspace_status(p.total(), workspace_dev, workspace_bytes)) return s;
+    const Cut c = grad_cut(Nout, K, M, true);
+    if (const lp_status s = workspace_status(c.sums, workspace_dev, workspace_bytes)) return s;
     clear_stale_error();
     GradArgs a = {};
     a.dy = (const __bf16 *)dy_dev;
@@ -1025,6 +1053,6 @@ extern "C" lp_status lp_ckpt8_fc_wgrad(int M, int K, int Nout, const void *dy_de
     a.J = K;
     a.C = M;
     a.blocks = (int)ckpt8_blocks((size_t)K);
-    gradient<true>(p, a, dwt, Sink{dw_dev, lddw, 0, nullptr, LP_ACT_NONE, accumulate != 0}, dbias_dev, (unsigned char *)workspace_dev, as_stream(stream));
+    gradient<true>(c, a, dwt, Sink{dw_dev, lddw, nullptr, dbias_dev, LP_ACT_NONE, accumulate != 0}, workspace_dev, as_stream(stream));
     return launch_status();
 }
