@@ -370,3 +370,20 @@ def test_calls_on_two_streams_with_workspaces_of_their_own():
                 lp.lp_mx4_fc_fwd(m, k, n, x, w[0], w[1], y, workspace=v)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, ys))
+
+
+# More tiles than compute units, and a few more: those few are cut along the reduction, the others are not
+@pytest.mark.parametrize("size", [(4328, 4096, 197), (777, 4096, 1219), (1092, 2048, 3606), (3954, 3000, 4300)])
+def test_forward_with_a_last_round_of_a_few_tiles(size):
+    check_fwd(*size, torch.bfloat16, "gelu", True, extra=3, yt=torch.float32)
+
+
+@pytest.mark.parametrize("size", [(4109, 388, 1500), (2771, 647, 1501), (4104, 1031, 1024), (4155, 4096, 2048)])
+def test_input_gradient_with_a_last_round_of_a_few_tiles(size):
+    check_dgrad(*size, torch.bfloat16, extra=3)
+
+
+@pytest.mark.parametrize("size", [(1024, 403, 4186), (1000, 645, 2725), (1024, 904, 4778), (2048, 4096, 4152)])
+def test_weight_gradient_with_a_last_round_of_a_few_tiles(size):
+    check_wgrad(*size, torch.bfloat16, True, accumulate=True, extra=3)
+    check_wgrad(*size, torch.float32, True)
