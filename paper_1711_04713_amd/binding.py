@@ -375,11 +375,13 @@ def _here(t, device, what, name):
 
 def _rows(t, rows, cols, device, what, name):
     """Address and row stride of a float tensor [rows][cols]."""
-    if t.shape != (rows, cols) or (cols > 1 and t.stride(1) != 1):
-        _refuse(what, "%s is not a [%d][%d] tensor with unit column stride" % (name, rows, cols))
-    if t.get_device() != device:
+    if t.shape == (rows, cols) and t.get_device() == device:
+        ld, step = t.stride()
+        if step == 1 or cols <= 1:
+            return t.data_ptr(), ld if rows > 1 else cols or 1
+    elif t.shape == (rows, cols):
         _refuse(what, "%s is not on the current GPU" % name)
-    return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, 1)
+    _refuse(what, "%s is not a [%d][%d] tensor with unit column stride" % (name, rows, cols))
 
 
 def _dense(t, nbytes, device, what, name):
@@ -391,14 +393,20 @@ def _dense(t, nbytes, device, what, name):
     return t.data_ptr()
 
 
+def _blocks(codes, scales, blocks, size, device, what, name):
+    """Addresses of a microscaled tensor's codes and scales."""
+    if (codes.nbytes == size * blocks and scales.nbytes == blocks and codes.is_contiguous() and scales.is_contiguous()
+            and codes.get_device() == device == scales.get_device()):
+        return codes.data_ptr(), scales.data_ptr()
+    return _dense(codes, size * blocks, device, what, name + "'s codes"), _dense(scales, blocks, device, what, name + "'s scales")
+
+
 def _mx4(codes, scales, rows, cols, device, what, name):
-    blocks = rows * ((cols + 255) // 256 * 8)
-    return _dense(codes, 16 * blocks, device, what, name + "'s codes"), _dense(scales, blocks, device, what, name + "'s scales")
+    return _blocks(codes, scales, rows * ((cols + 255) // 256 * 8), 16, device, what, name)
 
 
 def _ckpt8(codes, scales, rows, cols, device, what, name):
-    blocks = rows * ((cols + 31) // 32)
-    return _dense(codes, 32 * blocks, device, what, name + "'s codes"), _dense(scales, blocks, device, what, name + "'s scales")
+    return _blocks(codes, scales, rows * ((cols + 31) // 32), 32, device, what, name)
 
 
 def _vector(t, n, device, what, name):
