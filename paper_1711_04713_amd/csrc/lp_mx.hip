@@ -224,13 +224,17 @@ static void with_mode(lp_round r, F f)
 
 void mx4_quantize_launch(const void *x, lp_dtype xt, size_t rows, size_t cols, size_t ldx, void *codes, void *scales, hipStream_t st)
 {
-    PieceGrid g;
-    if (!piece_grid(rows, cols, mx4_blocks(cols), &g)) return; // (the caller's limits are narrower)
-    with_type(xt, [&](auto *tag) {
-        typedef std::remove_pointer_t<decltype(tag)> T;
-        hipLaunchKernelGGL((mx4_quantize_kernel<T, LP_ROUND_NEAREST_EVEN, false>), blocks_for(g), dim3(kThreads), 0, st, (const T *)x, ldx, g,
-                           (unsigned *)codes, (unsigned char *)scales, (uint64_t)0, (unsigned long long *)nullptr, (unsigned long long *)nullptr);
-    });
+    const size_t blocks = mx4_blocks(cols), most = (((size_t)1 << 31) - 1) / (blocks * 4); // rows of a launch
+    for (size_t r = 0; r < rows; r += most) {
+        PieceGrid g;
+        if (!piece_grid(std::min(rows - r, most), cols, blocks, &g)) return; // (a row has at most 2^24 columns)
+        with_type(xt, [&](auto *tag) {
+            typedef std::remove_pointer_t<decltype(tag)> T;
+            hipLaunchKernelGGL((mx4_quantize_kernel<T, LP_ROUND_NEAREST_EVEN, false>), blocks_for(g), dim3(kThreads), 0, st, (const T *)x + r * ldx, ldx, g,
+                               (unsigned *)codes + r * blocks * 4, (unsigned char *)scales + r * blocks, (uint64_t)0, (unsigned long long *)nullptr,
+                               (unsigned long long *)nullptr);
+        });
+    }
 }
 
 } // namespace lp

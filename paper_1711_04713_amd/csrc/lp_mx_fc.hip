@@ -627,7 +627,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     auto load_b = [&](int t) __attribute__((always_inline)) {
         constexpr int BLOCK = WEIGHTS ? 32 : 16;
         const long long left = std::min(std::max((long long)(end - t * 64) * a.blocks, 0LL), 0x07ffffffLL); // blocks
-        const int scales = __builtin_amdgcn_readfirstlane((int)left), codes = scales * BLOCK;
+        const int scales = __builtin_amdgcn_readfirstlane((int)left), codes = (int)((unsigned)scales * BLOCK);
         const size_t from = (size_t)t * 64 * a.blocks;
         raw.load(__builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.codes) + from * BLOCK, 0, codes, 0x00020000),
                  __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(a.scales) + from, 0, scales, 0x00020000), bat);

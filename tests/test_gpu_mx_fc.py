@@ -387,3 +387,17 @@ def test_input_gradient_with_a_last_round_of_a_few_tiles(size):
 def test_weight_gradient_with_a_last_round_of_a_few_tiles(size):
     check_wgrad(*size, torch.bfloat16, True, accumulate=True, extra=3)
     check_wgrad(*size, torch.float32, True)
+
+
+def test_forward_of_more_elements_than_one_quantizing_launch_takes():
+    m, k, n = (1 << 17) + 3, 1 << 17, 8                           # 2^34 elements and three rows more
+    rows = [0, m - 5, m - 4, m - 3, m - 2, m - 1]                 # the last three are the second launch's
+    x = torch.zeros((m, k), dtype=torch.bfloat16, device="cuda")
+    some = inputs(len(rows), k, torch.bfloat16, 1)
+    x[rows] = some.cuda()
+    w = weights(n, k, 2)
+    y = torch.full((m, n), 5.0, device="cuda")
+    run_fwd(m, k, n, x, w, y)
+    want, size = product(torch.from_numpy(mx.mx4_values(*mx.mx4_quantize(some.double().numpy())[:2], k)).cuda(), w[2].t())
+    mx.close(y[rows], want, mx.product_error(size, k), torch.float32)
+    assert not y[1:m - 5].any()
