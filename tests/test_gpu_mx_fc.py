@@ -401,3 +401,46 @@ def test_forward_of_more_elements_than_one_quantizing_launch_takes():
     want, size = product(torch.from_numpy(mx.mx4_values(*mx.mx4_quantize(some.double().numpy())[:2], k)).cuda(), w[2].t())
     mx.close(y[rows], want, mx.product_error(size, k), torch.float32)
     assert not y[1:m - 5].any()
+
+
+def test_gradients_of_more_than_2_32_elements():
+    m, k, n = (1 << 17) + 5, 40, (1 << 15) + 2
+    rows = [0, 77, m - 6, m - 5, m - 2, m - 1]
+    some = inputs(len(rows), n, torch.bfloat16, 3)
+    dy = torch.zeros((m, n), dtype=torch.bfloat16, device="cuda")
+    dy[rows] = some.cuda()
+    w = weights(n, k, 4)
+    dx = torch.full((m, k), 5.0, device="cuda")
+    lp.lp_mx4_fc_dgrad(m, k, n, dy, w[0], w[1], dx, workspace=workspace(lp.lp_mx4_fc_dgrad_workspace_bytes(m, k, n)))
+    want, size = product(some.cuda(), w[2])
+    mx.close(dx[rows], want, mx.product_error(size, n), torch.float32)
+    assert not dx[1:77].any() and not dx[78:m - 6].any()
+    x = kept(len(rows), k, 5)
+    codes, scales = ckpt8_buffers(m, k)
+    codes.zero_()
+    scales.fill_(127)
+    codes[rows], scales[rows] = x[0], x[1]
+    dw, db = torch.full((n, k), 5.0, device="cuda"), torch.empty(n, device="cuda")
+    lp.lp_ckpt8_fc_wgrad(m, k, n, dy, codes, scales, dw, dbias=db, workspace=workspace(lp.lp_ckpt8_fc_wgrad_workspace_bytes(m, k, n)))
+    want, size = product(some.cuda().t(), x[2])
+    mx.close(dw, want, mx.product_error(size, m), torch.float32)
+    mx.close(db, some.double().sum(0).numpy(), mx.product_error(some.double().abs().sum(0).numpy(), m), torch.float32)
+
+
+@pytest.mark.parametrize("ld", [(1 << 22) + 2, (1 << 22) + 1])
+def test_gradients_of_rows_far_apart(ld):
+    m, k, n = 35, 100, 70
+    dy = inputs(m, n, torch.bfloat16, 6)
+    wide = torch.full(((m - 1) * ld + n,), float("nan"), dtype=torch.bfloat16, device="cuda")   # what lies between is not used
+    d = wide.as_strided((m, n), (ld, 1))
+    d.copy_(dy)
+    w = weights(n, k, 7)
+    dx = torch.empty((m, k), device="cuda")
+    lp.lp_mx4_fc_dgrad(m, k, n, d, w[0], w[1], dx, workspace=workspace(lp.lp_mx4_fc_dgrad_workspace_bytes(m, k, n)))
+    want, size = product(dy.cuda(), w[2])
+    mx.close(dx, want, mx.product_error(size, n), torch.float32)
+    x = kept(m, k, 8)
+    dw = torch.empty((n, k), device="cuda")
+    lp.lp_ckpt8_fc_wgrad(m, k, n, d, x[0], x[1], dw, workspace=workspace(lp.lp_ckpt8_fc_wgrad_workspace_bytes(m, k, n)))
+    want, size = product(dy.cuda().t(), x[2])
+    mx.close(dw, want, mx.product_error(size, m), torch.float32)
