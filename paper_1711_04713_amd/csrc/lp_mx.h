@@ -33,36 +33,44 @@ inline unsigned piece_magic(unsigned d) { return d <= 1 ? 0xffffffffu : (unsigne
 typedef float v8f __attribute__((ext_vector_type(8)));
 typedef float v2f __attribute__((ext_vector_type(2)));
 
+template <int W>
+struct Floats {
+    typedef float V __attribute__((ext_vector_type(W)));
+};
 // One load or store of the whole vector at the element's own alignment (the memory system takes 16 bytes at
-// any address), or element by element where fewer than eight exist.
-template <typename T>
-__device__ __forceinline__ v8f load8(const T *p, int n)
+// any address), or element by element where fewer than W exist.
+template <int W, typename T>
+__device__ __forceinline__ typename Floats<W>::V load_floats(const T *p, int n)
 {
-    typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-    v8f v = 0.0f;
-    if (n >= 8) {
+    typedef T V __attribute__((ext_vector_type(W), aligned(sizeof(T))));
+    typename Floats<W>::V v = 0.0f;
+    if (n >= W) {
         const V t = *reinterpret_cast<const V *>(p);
-        v = __builtin_convertvector(t, v8f);
+        v = __builtin_convertvector(t, typename Floats<W>::V);
     } else {
 #pragma unroll
-        for (int j = 0; j < 7; ++j)
+        for (int j = 0; j < W - 1; ++j)
             if (j < n) v[j] = (float)p[j];
     }
     return v;
 }
-template <typename T>
-__device__ __forceinline__ void store8(T *p, int n, v8f v)
+template <int W, typename T>
+__device__ __forceinline__ void store_floats(T *p, int n, typename Floats<W>::V v)
 {
-    typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    typedef T V __attribute__((ext_vector_type(W), aligned(sizeof(T))));
     const V t = __builtin_convertvector(v, V);
-    if (n >= 8) {
+    if (n >= W) {
         *reinterpret_cast<V *>(p) = t;
     } else {
 #pragma unroll
-        for (int j = 0; j < 7; ++j)
+        for (int j = 0; j < W - 1; ++j)
             if (j < n) p[j] = t[j];
     }
 }
+template <typename T>
+__device__ __forceinline__ v8f load8(const T *p, int n) { return load_floats<8>(p, n); }
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int n, v8f v) { store_floats<8>(p, n, v); }
 
 // ------------------------------------------------------------- blocks of 32 in four neighbouring lanes
 
@@ -145,11 +153,12 @@ __device__ __forceinline__ float act_value(float h, lp_actfn f)
     return h;
 }
 
-__device__ __forceinline__ v8f act_values(v8f v, lp_actfn f)
+template <typename V>
+__device__ __forceinline__ V act_values(V v, lp_actfn f)
 {
     if (f != LP_ACT_NONE) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = act_value(v[j], f);
+        for (int j = 0; j < (int)(sizeof(V) / sizeof(float)); ++j) v[j] = act_value(v[j], f);
     }
     return v;
 }

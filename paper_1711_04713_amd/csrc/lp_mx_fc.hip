@@ -51,21 +51,21 @@ struct Sink {
     int accumulate;
 };
 
-// Eight neighbouring results of a row, n of which exist.
-template <typename T>
-__device__ __forceinline__ void put8(const Sink &s, T *to, const float *bias, int n, v8f v)
+// W neighbouring results of a row, n of which exist.
+template <int W, typename T>
+__device__ __forceinline__ void put(const Sink &s, T *to, const float *bias, int n, typename Floats<W>::V v)
 {
-    if (s.bias) v += load8(bias, n);
-    if (s.accumulate) v += load8(to, n);
-    store8(to, n, act_values(v, s.act));
+    if (s.bias) v += load_floats<W>(bias, n);
+    if (s.accumulate) v += load_floats<W>(to, n);
+    store_floats<W>(to, n, act_values(v, s.act));
 }
 
 // A wave's results, MB x NB blocks of 32 rows x 32 columns from (i0, j0) of a tile on, of which I x J exist: 32 rows at a time
-// through a piece of LDS of its own, so that they leave as whole rows, eight neighbours a lane.  In the accumulators a lane
-// holds, of row lane % 32 of a block, columns 8 g + 4 (lane / 32) + 0..3 in registers 4 g ..
+// through a piece of LDS of its own, so that they leave as whole rows, W neighbours a lane: 16 bytes, so that what the lanes of a
+// store write lies together.  In the accumulators a lane holds, of row lane % 32 of a block, columns 8 g + 4 (lane / 32) + 0..3 in registers 4 g ..
 constexpr int result_row(int NB) { return NB * 32 + 4; } // floats, padded
 constexpr int result_bytes(int NB) { return 32 * result_row(NB) * 4; }
-template <int MB, int NB, typename PUT>
+template <int MB, int NB, int W, typename PUT>
 __device__ __forceinline__ void put_blocks(float *mine, const v16f (&acc)[NB][MB], int i0, int j0, int I, int J, PUT put)
 {
     constexpr int ROW = result_row(NB);
@@ -82,12 +82,19 @@ __device__ __forceinline__ void put_blocks(float *mine, const v16f (&acc)[NB][MB
                 *(v4f *)(mine + l32 * ROW + j * 32 + 8 * g + 4 * h) = v4f{c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
             }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); // (one wave: its own writes are all there)
-#pragma unroll 2
-        for (int q = 0; q < 2 * NB; ++q) {
-            const int k = q * 64 + lane, row = k / (NB * 4), col = k % (NB * 4) * 8;
-            const v4f lo = *(const v4f *)(mine + row * ROW + col), hi = *(const v4f *)(mine + row * ROW + col + 4);
+#pragma unroll 4
+        for (int q = 0; q < 16 * NB / W; ++q) {
+            const int k = q * 64 + lane, row = k / (NB * 32 / W), col = k % (NB * 32 / W) * W;
+            const float *from = mine + row * ROW + col;
             const int i = ib + row, j = j0 + col;
-            if (i < I && j < J) put(i, j, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            typename Floats<W>::V v;
+#pragma unroll
+            for (int p = 0; p < W; p += 4) {
+                const v4f part = *(const v4f *)(from + p);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[p + e] = part[e];
+            }
+            if (i < I && j < J) put(i, j, v);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
@@ -144,15 +151,15 @@ __device__ __forceinline__ void put_results(const Grid &g, const Sink &out, cons
     const int ti = p.tile_i * TI, tj = p.tile_j * TJ;
     if (p.sums >= 0) {
         float *to = g.sums + p.sums * tile_sums(TI, TJ);
-        put_blocks<MB, NB>(mine, acc, i0, j0, I - ti, J - tj, [&](int i, int j, v8f v) __attribute__((always_inline)) {
-            *(v4f *)(to + i * TJ + j) = __builtin_shufflevector(v, v, 0, 1, 2, 3); // (whole pieces, where the row ends inside too)
-            *(v4f *)(to + i * TJ + j + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+        put_blocks<MB, NB, 4>(mine, acc, i0, j0, I - ti, J - tj, [&](int i, int j, v4f v) __attribute__((always_inline)) {
+            *(v4f *)(to + i * TJ + j) = v; // (whole pieces, where the row ends inside too)
         });
     } else {
         OutT *to = (OutT *)out.y + ti * out.ld + tj;
         const float *bias = out.bias + tj;
-        put_blocks<MB, NB>(mine, acc, i0, j0, I - ti, J - tj, [&](int i, int j, v8f v) __attribute__((always_inline)) {
-            put8(out, to + i * out.ld + j, bias + j, J - tj - j, v);
+        constexpr int W = 16 / sizeof(OutT);
+        put_blocks<MB, NB, W>(mine, acc, i0, j0, I - ti, J - tj, [&](int i, int j, typename Floats<W>::V v) __attribute__((always_inline)) {
+            put<W>(out, to + i * out.ld + j, bias + j, J - tj - j, v);
         });
     }
 }
@@ -183,7 +190,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const Grid g, Sink out,
     const int piece = within * 256 + threadIdx.x, row = piece / (TJ / 8), col = piece % (TJ / 8) * 8;
     const int i = p.tile_i * TI + row, j = p.tile_j * TJ + col;
     if (row < TI && i < I && j < J)
-        put8(out, (T *)out.y + i * out.ld + j, out.bias + j, J - j, joined(sums + row * TJ + col, [](const float *q) { return load8(q, 8); }));
+        put<8>(out, (T *)out.y + i * out.ld + j, out.bias + j, J - j, joined(sums + row * TJ + col, [](const float *q) { return load8(q, 8); }));
     const int r = p.tile_i * TI + threadIdx.x;
     if (out.db && p.tile_j == 0 && within == 0 && threadIdx.x < TI && r < I) {
         const float v = joined(sums + TI * TJ + threadIdx.x, [](const float *q) { return *q; });
@@ -434,7 +441,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void mx4_few_kernel(const Mx4Arg
         v8f sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < kFewWaves; ++k) sum += *(const v8f *)&sums[k][m][n - n0];
-        put8(a.out, (OutT *)a.out.y + m * a.out.ld + n, a.out.bias + n, a.N - n, sum);
+        put<8>(a.out, (OutT *)a.out.y + m * a.out.ld + n, a.out.bias + n, a.N - n, sum);
     }
 }
 
