@@ -164,7 +164,8 @@ __device__ __forceinline__ void put_results(const Grid &g, const Sink &out, cons
     }
 }
 
-// y = act(sum of the parts + bias), db the same of the rows' sums: a thread takes eight neighbours of a row of a tile
+// y = act(sum of the parts + bias), db the same of the rows' sums: a thread takes kJoinW neighbours of a row of a tile
+constexpr int kJoinW = 4; // (16 bytes of each part, so that a load's lanes lie together)
 template <typename T>
 __global__ __launch_bounds__(256) void join_parts_kernel(const Grid g, Sink out, int TI, int TJ, int I, int J, int per_tile)
 {
@@ -187,10 +188,10 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const Grid g, Sink out,
         for (; k < g.parts; ++k) v += load(q + k * part);
         return v;
     };
-    const int piece = within * 256 + threadIdx.x, row = piece / (TJ / 8), col = piece % (TJ / 8) * 8;
+    const int piece = within * 256 + threadIdx.x, row = piece / (TJ / kJoinW), col = piece % (TJ / kJoinW) * kJoinW;
     const int i = p.tile_i * TI + row, j = p.tile_j * TJ + col;
     if (row < TI && i < I && j < J)
-        put<8>(out, (T *)out.y + i * out.ld + j, out.bias + j, J - j, joined(sums + row * TJ + col, [](const float *q) { return load8(q, 8); }));
+        put<kJoinW>(out, (T *)out.y + i * out.ld + j, out.bias + j, J - j, joined(sums + row * TJ + col, [](const float *q) { return *(const v4f *)q; }));
     const int r = p.tile_i * TI + threadIdx.x;
     if (out.db && p.tile_j == 0 && within == 0 && threadIdx.x < TI && r < I) {
         const float v = joined(sums + TI * TJ + threadIdx.x, [](const float *q) { return *q; });
@@ -846,7 +847,7 @@ static void with_type(lp_dtype t, F f)
 // out = act(sum of the parts + bias)
 static void join_parts(const Cut &c, const Grid &g, lp_dtype t, const Sink &out, int I, int J, hipStream_t st)
 {
-    const int per_tile = (std::min(c.i, I) * (c.j / 8) + 255) / 256;
+    const int per_tile = (std::min(c.i, I) * (c.j / kJoinW) + 255) / 256;
     with_type(t, [&](auto *tag) {
         typedef std::remove_pointer_t<decltype(tag)> T;
         hipLaunchKernelGGL(join_parts_kernel<T>, dim3((unsigned)g.rest * per_tile), dim3(256), 0, st, g, out, c.i, c.j, I, J, per_tile);
