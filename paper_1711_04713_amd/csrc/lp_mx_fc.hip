@@ -786,6 +786,9 @@ constexpr TileCost kMx4Tiles[4] = {{64, 64, 0.23, 0.215, 1.85, 0.85}, {128, 128,
 // 64 x 128, 128 x 128, 256 x 256; a stage is 64 positions
 constexpr TileCost kInputTiles[3] = {{64, 128, 0.39, 0.315, 2.65, 0.45}, {128, 128, 0.505, 0.455, 3.15, 0.0}, {256, 256, 1.19, 1.34, 4.1, 0.0}};
 constexpr TileCost kWeightTiles[3] = {{64, 128, 0.91, 0.405, 4.75, 0.65}, {128, 128, 0.77, 0.535, 4.95, 1.75}, {256, 256, 1.265, 1.51, 8.5, 6.1}};
+// The same where Nout is odd: every other row of a dense dY starts inside a word, and all of it goes through registers.  (By the
+// other table: 601 x 768 over 256 rows 12.6 us instead of 8.9, 4097 x 4096 over 4096 248 instead of 200.)
+constexpr TileCost kOddWeightTiles[3] = {{64, 128, 0.715, 0.485, 3.75, 0.45}, {128, 128, 1.1, 0.675, 5.1, 1.25}, {256, 256, 1.64, 1.57, 8.0, 3.05}};
 
 // How a product I x J with `stages` stages of its reduction is cut into workgroups.
 struct Cut {
@@ -795,8 +798,8 @@ struct Cut {
     double us;
 };
 
-// The cheapest of the tiles and numbers of parts, by an estimate that the tables above were fitted to (2102 timings of 268
-// problems: the choice costs 0.7 % on the average; it is a part too many or too few, 10 to 30 % of 5 to 15 us, where it is
+// The cheapest of the tiles and numbers of parts, by an estimate that the tables above were fitted to (2373 timings of 324
+// problems: the choice costs 1.2 % on the average; it is a part too many or too few, 10 to 30 % of 5 to 15 us, where it is
 // worst).  Results leave at 44 GB/s a compute unit; joining the parts is a launch, and their sums go through memory at
 // 7.5 TB/s.  A part has `step` stages or a multiple of them, and `least` at least.
 template <int SIZES>
@@ -911,7 +914,7 @@ static void few_launch(const Mx4Args &a, const void *x, lp_dtype xt, size_t ldx,
 
 static Cut grad_cut(int I, int J, int C, bool weights)
 {
-    return cut_product(I, J, std::max((C + 63) / 64, 1), 1, 4, weights ? kWeightTiles : kInputTiles, 4);
+    return cut_product(I, J, std::max((C + 63) / 64, 1), 1, 4, !weights ? kInputTiles : I % 2 ? kOddWeightTiles : kWeightTiles, 4);
 }
 
 template <bool WEIGHTS, typename T>
