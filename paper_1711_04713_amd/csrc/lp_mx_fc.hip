@@ -541,6 +541,19 @@ struct RawBlock {
     }
 };
 
+// The eight from column `col` on of a row of `cols`, 8 at least; zeros where it has ended.  One load, that lies within the row,
+// and a shift.
+__device__ __forceinline__ v4u load_tail(const __bf16 *row, int col, int cols)
+{
+    typedef unsigned short V __attribute__((ext_vector_type(8), aligned(2)));
+    const int from = min(col, cols - 8), gone = col - from;
+    v4u v = __builtin_bit_cast(v4u, *reinterpret_cast<const V *>(row + from));
+    if (gone & 1) v = v4u{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+    if (gone & 2) v = v4u{v[1], v[2], v[3], 0};
+    if (gone & 4) v = v4u{v[2], v[3], 0, 0};
+    return gone >= 8 ? v4u{0, 0, 0, 0} : v;
+}
+
 template <int MB, int NB, int WM, int WN, bool WEIGHTS, bool WORDS, typename OutT>
 __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs a)
 {
@@ -604,15 +617,27 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
             else raw_dy[q] = __builtin_bit_cast(v4u, *reinterpret_cast<const V *>(a.dy + (WEIGHTS ? std::min(from, end - 8) : from)));
         }
     };
-    // the same at once, a piece at a time
+    // The ragged stage, at once: as many pieces on their way together as there are registers for beside the sums.
     auto bring_dy = [&](int t, int buf) __attribute__((always_inline)) {
+        constexpr int TOGETHER = MB * NB >= 8 ? 1 : PER;
+        const int rows = WEIGHTS ? a.C : a.I, cols = WEIGHTS ? a.I : a.C;
 #pragma unroll 1
-        for (int k = threadIdx.x; k < PER * THREADS; k += THREADS) {
-            const int r = k / (AROW / 16), s = k % (AROW / 16), to = WEIGHTS ? ((s >> 2) ^ (r & ATURN)) * 4 + (s & 3) : s ^ (r & 7);
-            const int row = WEIGHTS ? t * 64 + r : i0 + r, col = WEIGHTS ? i0 + s * 8 : t * 64 + s * 8;
-            const v4u piece = load_piece(a.dy + row * a.ld + col, row < (WEIGHTS ? a.C : a.I) ? (WEIGHTS ? a.I : a.C) - col : 0);
+        for (int q0 = 0; q0 < PER; q0 += TOGETHER) {
+            v4u piece[TOGETHER];
+#pragma unroll
+            for (int q = 0; q < TOGETHER; ++q) {
+                const int k = (q0 + q) * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
+                const int row = WEIGHTS ? t * 64 + r : i0 + r, col = WEIGHTS ? i0 + s * 8 : t * 64 + s * 8;
+                if (rows < 1 || cols < 8) piece[q] = load_piece(a.dy + row * a.ld + col, row < rows ? cols - col : 0);
+                else piece[q] = load_tail(a.dy + min(row, rows - 1) * a.ld, row < rows ? col : cols, cols);
+            }
             __builtin_amdgcn_s_waitcnt(0); // (and the zeros of the empty loads have arrived)
-            *(v4u *)(lds + buf * STAGE + r * AROW + to * 16) = piece;
+#pragma unroll
+            for (int q = 0; q < TOGETHER; ++q) {
+                const int k = (q0 + q) * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
+                const int to = WEIGHTS ? ((s >> 2) ^ (r & ATURN)) * 4 + (s & 3) : s ^ (r & 7);
+                *(v4u *)(lds + buf * STAGE + r * AROW + to * 16) = piece[q];
+            }
         }
     };
     auto place_dy = [&](int buf) __attribute__((always_inline)) {
@@ -727,7 +752,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     load_dy(first, 0, L0, L2);
     place_b(0, 0, 4);
     load_b(first + 1);
-    if (!WORDS || whole == first) bring_dy(first, 0);
+    if (whole == first) {
+        bring_dy(first, 0);
+    } else if constexpr (!WORDS) {
+        fetch_dy(first);
+        place_dy(0);
+    }
     if constexpr (!WORDS) fetch_dy(first + 1);
     all_arrived();
     load_dy(first + 1, 1, L0, L1);
