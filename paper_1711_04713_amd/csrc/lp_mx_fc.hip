@@ -456,7 +456,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void mx4_few_kernel(const Mx4Arg
 // A workgroup owns TI x TJ results, a wave MB x NB blocks of 32 x 32; a stage is 64 positions of the reduction in one of two
 // LDS buffers.  B's codes pass through registers, a block of 32 a thread, and are decoded one stage ahead; dY
 // comes by loads to LDS (or, where its rows do not start on words, through registers like the codes: 200 x 4096 from 1001
-// columns 13.6 us, from 1002 12.8; 8192 x 4096 from 14337 1020, from 14338 800).  The matrix
+// columns 13.0 us, from 1002 12.5; 8192 x 4096 from 14337 1020, from 14338 750).  The matrix
 // instruction wants eight neighbouring positions of a row or column in a lane: those of dY's rows lie together in memory
 // (16-byte piece p of row r at place p ^ (r % 8), as above); tiles with the reduction along their rows are read by
 // ds_read_b64_tr_b16, which hands each of 16 lanes four rows' elements of its column.  Their rows are 512 (or 256) bytes, so
@@ -485,6 +485,8 @@ __device__ __forceinline__ v8s read_columns(const unsigned char *__restrict__ fi
     const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV4)first), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV4)next);
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
+
+constexpr size_t kNearRows = (size_t)1 << 22; // dY's row strides up to which a tile's offsets fit 32 bits
 
 // n (at most 8) bfloat16 of a row as one 16-byte piece, zeros behind them
 __device__ __forceinline__ v4u load_piece(const __bf16 *p, int n)
@@ -572,14 +574,20 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, h = lane >> 5, wm = wave % WM, wn = wave / WM;
 
-    // dY.  The last stage of the whole reduction comes element by element through registers where it, or a row, ends inside a
-    // piece: what lies behind must not be multiplied, not even by zero.
+    // dY.  The last stage of the whole reduction comes through registers where it, or a row, ends inside a piece: what lies
+    // behind must not be multiplied, not even by zero.
     const bool ragged = last == a.grid.stages && (last * 64 != a.C || (WEIGHTS && i0 + TI > a.I));
-    const int whole = last - ragged; // stages first .. whole - 1 come in whole pieces
+    // Stages first .. whole - 1 come in whole pieces.  (Through registers only where offsets are 32 bits, and a piece reaches no
+    // further than into the next row.)
+    const bool direct = WORDS || (a.ld < kNearRows && (!WEIGHTS || a.ld >= 8));
+    const int whole = direct ? last - ragged : first;
     unsigned at[PER];
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
-        if constexpr (WEIGHTS) {
+        if constexpr (!WORDS) {
+            const int k = q * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
+            at[q] = (unsigned)(WEIGHTS ? r : min(r, a.I - 1 - i0)) * (unsigned)(a.ld * 2) + s * 16;
+        } else if constexpr (WEIGHTS) {
             constexpr int LANES = AROW / 16; // of a row
             const int r = (wave * PER + q) * (64 / LANES) + lane / LANES, s = lane % LANES;
             at[q] = (unsigned)r * (unsigned)(a.ld * 2) + (((s >> 2) ^ (r & ATURN)) * 4 + (s & 3)) * 16;
@@ -602,22 +610,23 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
             for (int q = decltype(from)::value; q < decltype(to)::value; ++q) load_lds16(rsrc, lds + buf * STAGE + (wave * PER + q) * 1024, at[q], 0);
         }
     };
-    v4u raw_dy[PER] = {};
-    auto fetch_dy = [&](int t) __attribute__((always_inline)) {
+    // A thread's pieces of a stage at once, or in two halves where registers are short beside a large tile's sums.  (8192 x 4096
+    // from 14337: 1.21 ms at once, 1.02 in halves; weights 14337 x 4096 over 8192: 0.99, 1.04.)
+    constexpr int HALF = MB * NB >= 8 && !WEIGHTS ? PER / 2 : PER;
+    v4u raw_dy[HALF] = {};
+    auto fetch_dy = [&](int t, int half) __attribute__((always_inline)) {
         if (t >= whole) return;
         typedef unsigned short V __attribute__((ext_vector_type(8), aligned(2)));
-        // (weights: a row's last piece reaches into the next row; the last row is not brought this way)
-        const size_t end = (size_t)(a.C - 1) * a.ld + a.I;
+        const size_t from = WEIGHTS ? (size_t)t * 64 * a.ld + i0 : (size_t)i0 * a.ld + t * 64;
+        // (weights: a row's last piece reaches into the next row, the tile's into the one behind, but not past the end)
+        const unsigned most = WEIGHTS ? (unsigned)std::min(((size_t)(a.C - 1) * a.ld + a.I - 8 - from) * 2, (size_t)0x7ffffffe) : 0;
 #pragma unroll
-        for (int q = 0; q < PER; ++q) {
-            const int k = q * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
-            const int row = WEIGHTS ? t * 64 + r : min(i0 + r, a.I - 1), col = WEIGHTS ? i0 + s * 8 : t * 64 + s * 8;
-            const size_t from = row * a.ld + col;
-            if (WEIGHTS && a.ld < 8) raw_dy[q] = load_piece(a.dy + from, a.I - col);
-            else raw_dy[q] = __builtin_bit_cast(v4u, *reinterpret_cast<const V *>(a.dy + (WEIGHTS ? std::min(from, end - 8) : from)));
+        for (int q = 0; q < HALF; ++q) {
+            const unsigned o = at[half * HALF + q];
+            raw_dy[q] = __builtin_bit_cast(v4u, *reinterpret_cast<const V *>(reinterpret_cast<const char *>(a.dy + from) + (WEIGHTS ? std::min(o, most) : o)));
         }
     };
-    // The ragged stage, at once: as many pieces on their way together as there are registers for beside the sums.
+    // A stage at once, the ragged one for instance: as many pieces on their way together as there are registers for beside the sums.
     auto bring_dy = [&](int t, int buf) __attribute__((always_inline)) {
         constexpr int TOGETHER = MB * NB >= 8 ? 1 : PER;
         const int rows = WEIGHTS ? a.C : a.I, cols = WEIGHTS ? a.I : a.C;
@@ -640,10 +649,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
             }
         }
     };
-    auto place_dy = [&](int buf) __attribute__((always_inline)) {
+    auto place_dy = [&](int buf, int half) __attribute__((always_inline)) {
 #pragma unroll
-        for (int q = 0; q < PER; ++q) {
-            const int k = q * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
+        for (int q = 0; q < HALF; ++q) {
+            const int k = (half * HALF + q) * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
             const int to = WEIGHTS ? ((s >> 2) ^ (r & ATURN)) * 4 + (s & 3) : s ^ (r & 7);
             *(v4u *)(lds + buf * STAGE + r * AROW + to * 16) = raw_dy[q];
         }
@@ -732,17 +741,25 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
         load_dy(t + 1, B ^ 1, L1, L2);
         place_b(B ^ 1, 0, 2);
         LP_STEP(0)
+        if constexpr (!WORDS && HALF < PER) {
+            place_dy(B ^ 1, 0);
+            fetch_dy(t + 1, 1);
+        }
         fragments(B, 2);
         place_b(B ^ 1, 2, 4);
         load_b(t + 2);
         LP_STEP(1)
-        if constexpr (!WORDS) {
-            place_dy(B ^ 1);
-            fetch_dy(t + 2);
+        if constexpr (!WORDS && HALF == PER) {
+            place_dy(B ^ 1, 0);
+            fetch_dy(t + 2, 0);
         }
         fragments(B, 3);
         LP_STEP(2)
-        if (ragged && t + 2 == last) bring_dy(t + 1, B ^ 1);
+        if constexpr (!WORDS && HALF < PER) {
+            place_dy(B ^ 1, 1);
+            fetch_dy(t + 2, 0);
+        }
+        if (t + 1 >= whole && t + 1 < last) bring_dy(t + 1, B ^ 1);
         arrived_but<LATER>();
         fragments(B ^ 1, 0);
         load_dy(t + 2, B, L0, L1);
@@ -755,10 +772,12 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     if (whole == first) {
         bring_dy(first, 0);
     } else if constexpr (!WORDS) {
-        fetch_dy(first);
-        place_dy(0);
+        for (int half = 0; half < PER / HALF; ++half) {
+            fetch_dy(first, half);
+            place_dy(0, half);
+        }
     }
-    if constexpr (!WORDS) fetch_dy(first + 1);
+    if constexpr (!WORDS) fetch_dy(first + 1, 0);
     all_arrived();
     load_dy(first + 1, 1, L0, L1);
     fragments(0, 0);
@@ -952,7 +971,7 @@ static void grad_launch(const Cut &c, const GradArgs &a, hipStream_t st)
 {
     const dim3 grid(workgroups(a.grid));
     // Loads to LDS ask for words, and reach 2^31 bytes from a tile's first row.
-    const bool words = aligned_to(a.dy, 4) && a.ld % 2 == 0 && a.ld < ((size_t)1 << 22);
+    const bool words = aligned_to(a.dy, 4) && a.ld % 2 == 0 && a.ld < kNearRows;
 #define LP_TILES(MB, NB, WM, WN)                                                                                                             \
     hipLaunchKernelGGL((words ? gradient_kernel<MB, NB, WM, WN, WEIGHTS, true, T> : gradient_kernel<MB, NB, WM, WN, WEIGHTS, false, T>), grid, \
                        dim3(WM * WN * 64), 0, st, a)
