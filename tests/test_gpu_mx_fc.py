@@ -157,7 +157,7 @@ def check_wgrad(m, k, n, dwt, with_bias, accumulate=False, extra=-1):
     junk_is_left(wide, k)
 
 
-@pytest.mark.parametrize("size", SIZES + [(0, 70, 40), (4000, 200, 136), (1000, 64, 2), (300, 500, 6), (129, 33, 1)])
+@pytest.mark.parametrize("size", SIZES + [(0, 70, 40), (4000, 200, 136), (1000, 64, 2), (300, 500, 6), (129, 33, 1), (200, 40, 7), (64, 300, 5)])
 def test_weight_gradient(size):
     check_wgrad(*size, torch.float32, True)
     check_wgrad(*size, torch.bfloat16, True, accumulate=True, extra=3)
@@ -427,9 +427,10 @@ def test_gradients_of_more_than_2_32_elements():
     mx.close(db, some.double().sum(0).numpy(), mx.product_error(some.double().abs().sum(0).numpy(), m), torch.float32)
 
 
+@pytest.mark.parametrize("m", [35, 130])
 @pytest.mark.parametrize("ld", [(1 << 22) + 2, (1 << 22) + 1])
-def test_gradients_of_rows_far_apart(ld):
-    m, k, n = 35, 100, 70
+def test_gradients_of_rows_far_apart(ld, m):
+    k, n = 100, 70
     dy = inputs(m, n, torch.bfloat16, 6)
     wide = torch.full(((m - 1) * ld + n,), float("nan"), dtype=torch.bfloat16, device="cuda")   # what lies between is not used
     d = wide.as_strided((m, n), (ld, 1))
