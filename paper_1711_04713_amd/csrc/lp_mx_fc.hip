@@ -22,10 +22,6 @@ __device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t from, unsigned
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (LdsPtr)to, 16, lane_offset, offset, 0, 0);
 }
-__device__ __forceinline__ void load_lds4(__amdgpu_buffer_rsrc_t from, unsigned char *to, unsigned lane_offset, int offset)
-{
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (LdsPtr)to, 4, lane_offset, offset, 0, 0);
-}
 
 // Everything that this wave has asked for has arrived but the last LATER loads from memory, and so it is in every other wave of
 // the workgroup.
@@ -228,8 +224,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
     constexpr int TM = MB * 32 * WM, TN = NB * 32 * WN, WAVES = WM * WN, ROWS = TM + TN, STAGE = ROWS * 128, PER = ROWS / 8 / WAVES;
     constexpr int SROWS = ROWS / WAVES, SPER = SROWS / 32; // rows whose scale bytes a wave brings, loads that takes
     static_assert(TM % SROWS == 0, "of one tensor");
-    // (the scale bytes of a row's stages that do not exist are read too, from whatever follows: 32 bytes more)
-    __shared__ __align__(1024) unsigned char lds[BUFFERS * STAGE + ROWS * 32 + 32];
+    __shared__ __align__(1024) unsigned char lds[BUFFERS * STAGE + ROWS * 32];
     static_assert(WAVES * result_bytes(NB) <= (int)sizeof(lds), "results pass through the same memory");
     Place p;
     if (!find_place(a.grid, &p)) return;
@@ -263,40 +258,39 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
     constexpr std::integral_constant<int, 3 * PER / 8> L1;
     constexpr std::integral_constant<int, 6 * PER / 8> L2;
     constexpr std::integral_constant<int, PER> L3;
-    // Scale bytes of stages t .. t + 3 (t a multiple of 4), 32 for each row, two lanes a row; where a row ends before that its last
-    // 32.  Rows of fewer than 32 come a word a lane: the rows' eight bytes of the first stage, then those of the next.
+    // Scale bytes of stages t .. t + 3 (t a multiple of 4), 32 for each row: of 32 rows the first 16 each, then the others, so
+    // that a read's lanes lie side by side.  (A row's 32 bytes together, read a word at a time, cost half of all LDS cycles.)
+    // Bytes of stages that do not exist are the next row's, or zeros behind the last: the descriptor ends with the tensor.
     unsigned char *const scales = lds + BUFFERS * STAGE;
-    const bool narrow = a.blocks < 32;
-    const int row_step = narrow ? 8 : 32, stage_step = narrow ? ROWS * 8 : 8;
-    auto scales_of = [&](int size) __attribute__((always_inline)) {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(wave * SROWS < TM ? a.xs + (size_t)m0 * a.blocks : a.ws + (size_t)n0 * a.blocks), 0,
-                                                 size, 0x00020000);
-    };
+    const bool of_x = wave * SROWS < TM;
     unsigned scale_at[SPER];
 #pragma unroll
-    for (int i = 0; i < SPER; ++i) scale_at[i] = row_of(wave * SROWS + i * 32 + lane / 2) * (unsigned)a.blocks + (lane & 1) * 16;
+    for (int i = 0; i < SPER; ++i) scale_at[i] = row_of(wave * SROWS + i * 32 + l32) * (unsigned)a.blocks + h * 16;
     auto load_scales = [&](int t) __attribute__((always_inline)) {
-        const __amdgpu_buffer_rsrc_t from = scales_of(__builtin_amdgcn_readfirstlane(t < last ? -1 : 0));
+        const unsigned char *base = (of_x ? a.xs + (size_t)m0 * a.blocks : a.ws + (size_t)n0 * a.blocks) + 8 * t;
+        const long long rest = (long long)(of_x ? a.M - m0 : a.N - n0) * a.blocks - 8 * t;
+        const int size = __builtin_amdgcn_readfirstlane(t < last ? (int)(unsigned)std::min(rest, 0xffffffffLL) : 0);
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(base), 0, size, 0x00020000);
 #pragma unroll
-        for (int i = 0; i < SPER; ++i) load_lds16(from, scales + wave * SROWS * 32 + i * 1024, scale_at[i], min(8 * t, a.blocks - 32));
-    };
-    auto load_narrow_scales = [&]() __attribute__((always_inline)) {
-        const __amdgpu_buffer_rsrc_t from = scales_of(-1);
-        for (int q = 0; q < last; ++q)
-#pragma unroll
-            for (int i = 0; i < SPER; ++i)
-                load_lds4(from, scales + q * ROWS * 8 + wave * SROWS * 8 + i * 256, row_of(wave * SROWS + i * 32 + lane / 2) * (unsigned)a.blocks + 4 * (lane & 1), 8 * q);
+        for (int i = 0; i < SPER; ++i) load_lds16(from, scales + wave * SROWS * 32 + i * 1024, scale_at[i], 0);
     };
     int xscale[4][MB], wscale[4][NB];
-    auto take_scales = [&](int t) __attribute__((always_inline)) {
-        const int moved = narrow ? 0 : max(8 * t - (a.blocks - 32), 0);
+    auto take_scales = [&]() __attribute__((always_inline)) {
+        auto take = [&](int block, int q) __attribute__((always_inline)) { return *(const v4i *)(scales + block * 1024 + q / 2 * 512 + l32 * 16); };
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const unsigned char *from = scales + moved + 4 * h + q * stage_step;
+        for (int q = 0; q < 4; q += 2) {
 #pragma unroll
-            for (int i = 0; i < MB; ++i) xscale[q][i] = *(const int *)(from + ((wm * MB + i) * 32 + l32) * row_step);
+            for (int i = 0; i < MB; ++i) {
+                const v4i v = take(wm * MB + i, q);
+                xscale[q][i] = h ? v[1] : v[0];
+                xscale[q + 1][i] = h ? v[3] : v[2];
+            }
 #pragma unroll
-            for (int i = 0; i < NB; ++i) wscale[q][i] = *(const int *)(from + (TM + (wn * NB + i) * 32 + l32) * row_step);
+            for (int i = 0; i < NB; ++i) {
+                const v4i v = take(TM / 32 + wn * NB + i, q);
+                wscale[q][i] = h ? v[1] : v[0];
+                wscale[q + 1][i] = h ? v[3] : v[2];
+            }
         }
     };
     v16f acc[NB][MB] = {};
@@ -348,15 +342,14 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Ar
         LP_STEP(Q, 3, true)
     };
 #undef LP_STEP
-    if (narrow) load_narrow_scales();
-    else load_scales(first);
+    load_scales(first);
 #pragma unroll
     for (int b = 0; b < BUFFERS - 1; ++b) stage(first + b, b, L0, L3);
     arrived_but<(BUFFERS - 2) * PER>();
     stage(first + BUFFERS - 1, BUFFERS - 1, L0, L1);
     fragments(0, 0);
     for (int t = first;; t += 4) {
-        take_scales(t);
+        take_scales();
         whole_stage(t, std::integral_constant<int, 0>());
         if (t + 1 >= last) break;
         whole_stage(t + 1, std::integral_constant<int, 1>());
