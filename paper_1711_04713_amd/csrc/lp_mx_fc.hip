@@ -210,6 +210,11 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const Grid g, Sink out,
 // come the same way, those of four stages at a time.
 //
 // Weights are the row operand: a lane ends up with four neighbouring columns of one row of y.
+//
+// Measured with codes in hand: 8192 x 14336 from 4096 245 to 260 us, 3.7 to 3.9 PFLOP/s (x in bfloat16: 345 to 360 with its
+// quantization and in a long run, where the clock falls to 1.3 GHz: the chip's power, not its pipes, bounds the large tiles); 256 x 4096 from
+// 25088 28.8 us, 64 x 4096 from 4096 7.2: tiles of 64 rows are bound by their loads (0.2 us for 16 KB a stage and unit) and,
+// alone on a unit, by the chain of a stage's barrier, reads and products.
 struct Mx4Args {
     const unsigned char *xc, *xs, *wc, *ws;
     int M, N, K, blocks;
@@ -457,6 +462,10 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void mx4_few_kernel(const Mx4Arg
 // codes also swap neighbouring 16 bytes where (column / 128 + row) is odd, for the sake of the writes.
 //
 // B is the row operand of the instruction, so that a lane ends up with four neighbouring columns of one row of D.
+//
+// Measured: 8192 x 4096 from 14336 730 to 760 us, 1.27 to 1.32 PFLOP/s; weights 14336 x 4096 over 8192 845 to 870, 1.11 to
+// 1.14 (a library product of two bfloat16 tensors of these sizes reaches 1.2 to 1.5).  A stage of the large tile takes 3170 cycles at
+// 1.7 GHz, 2384 without the decoding (2048 are the products'); 256 x 4096 weights over 256 rows 22 us: 16.8 MB leave at 3 TB/s.
 struct GradArgs {
     const __bf16 *dy;
     size_t ld;
@@ -824,7 +833,7 @@ static double stage_cost(const TileCost &c, long long work)
 }
 // 64 x 64, 128 x 128 (four buffers each), 256 x 256 (two), 128 x 128 with two, which lets two workgroups of a unit work and end
 // side by side; a stage is 256 positions
-constexpr TileCost kMx4Tiles[4] = {{64, 64, 0.23, 0.215, 1.85, 0.85}, {128, 128, 0.43, 0.555, 3.3, 2.9}, {256, 256, 1.3, 1.67, 4.8, 2.0}, {128, 128, 0.62, 0.525, 2.55, 1.3}};
+constexpr TileCost kMx4Tiles[4] = {{64, 64, 0.175, 0.2, 1.9, 0.8}, {128, 128, 0.345, 0.51, 3.35, 2.85}, {256, 256, 1.03, 1.58, 4.9, 3.2}, {128, 128, 0.54, 0.49, 2.6, 1.35}};
 // 64 x 128, 128 x 128, 256 x 256; a stage is 64 positions
 constexpr TileCost kInputTiles[3] = {{64, 128, 0.39, 0.315, 2.65, 0.45}, {128, 128, 0.505, 0.455, 3.15, 0.0}, {256, 256, 1.19, 1.34, 4.1, 0.0}};
 constexpr TileCost kWeightTiles[3] = {{64, 128, 0.91, 0.405, 4.75, 0.65}, {128, 128, 0.77, 0.535, 4.95, 1.75}, {256, 256, 1.265, 1.51, 8.5, 6.1}};
@@ -916,7 +925,7 @@ static Mx4Plan mx4_plan(int M, int K, int Nout)
     if (M <= 16) {
         // Few rows: every workgroup reads 16 rows of w and all of x, 8 TB/s in all, a wave's chunk takes half a microsecond.
         // Quantizing x is a launch of 2.3 us, or 0.35 us a row and chunk where every wave does it.
-        // us, few rows : tiles, bf16: 1 x 4096 -> 4096 4.2 : 10, 16 rows 7.0 : 10, 16 x 4096 -> 14336 13.5 : 10.8
+        // us, few rows : tiles, bf16: 1 x 4096 -> 4096 4.1 : 8.6, 16 rows 7.2 : 8.6, 16 x 4096 -> 14336 13.5 : 8.8
         const double chunks = (double)((p.blocks + 16 * kFewWaves - 1) / (16 * kFewWaves));
         const double read = (double)Nout * p.blocks * 17 * (1 + M / 16.0) / 8e6, few = 3.0 + std::max(0.5 * chunks, read);
         const double within = 0.35 * M * chunks;
