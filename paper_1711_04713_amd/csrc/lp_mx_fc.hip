@@ -223,7 +223,7 @@ struct Mx4Args {
 };
 
 template <int MB, int NB, int WM, int WN, int BUFFERS, typename OutT>
-__global__ __launch_bounds__(WM *WN * 64, 2) void mx4_product_kernel(const Mx4Args a)
+__global__ __launch_bounds__(WM *WN * 64, WM *WN == 4 && MB * NB * BUFFERS == 16 ? 1 : 2) void mx4_product_kernel(const Mx4Args a)
 {
     static_assert(BUFFERS == 2 || BUFFERS == 4, "a stage's buffer is known where it is written out");
     constexpr int TM = MB * 32 * WM, TN = NB * 32 * WN, WAVES = WM * WN, ROWS = TM + TN, STAGE = ROWS * 128, PER = ROWS / 8 / WAVES;
@@ -921,17 +921,22 @@ static Mx4Plan mx4_plan(int M, int K, int Nout)
 {
     Mx4Plan p = {};
     p.blocks = mx4_blocks((size_t)K);
-    p.cut = cut_product(M, Nout, (int)(p.blocks / 8), 4, 4, kMx4Tiles, 2);
+    double few_us = 0.0, few_floats = 0.0;
     if (M <= 16) {
         // Few rows: every workgroup reads 16 rows of w and all of x, 8 TB/s in all, a wave's chunk takes half a microsecond.
         // Quantizing x is a launch of 2.3 us, or 0.35 us a row and chunk where every wave does it.
         // us, few rows : tiles, bf16: 1 x 4096 -> 4096 4.1 : 8.6, 16 rows 7.2 : 8.6, 16 x 4096 -> 14336 13.5 : 8.8
         const double chunks = (double)((p.blocks + 16 * kFewWaves - 1) / (16 * kFewWaves));
-        const double read = (double)Nout * p.blocks * 17 * (1 + M / 16.0) / 8e6, few = 3.0 + std::max(0.5 * chunks, read);
-        const double within = 0.35 * M * chunks;
-        p.few = few + std::min(within, 2.3) < p.cut.us + 2.3;
-        p.floats = p.few && within < 2.8;
+        const double read = (double)Nout * p.blocks * 17 * (1 + M / 16.0) / 8e6;
+        few_floats = 0.35 * M * chunks;
+        few_us = 3.0 + std::max(0.5 * chunks, read) + std::min(few_floats, 2.3);
+        p.few = few_us < 2.5 + kMx4Tiles[0].ends + 2.3; // (what no tiles go below; an estimate of them takes half a microsecond)
     }
+    if (!p.few) {
+        p.cut = cut_product(M, Nout, (int)(p.blocks / 8), 4, 4, kMx4Tiles, 2);
+        p.few = M <= 16 && few_us < p.cut.us + 2.3;
+    }
+    p.floats = p.few && few_floats < 2.8;
     if (p.few) p.cut = Cut{};
     if (p.floats) return p;
     p.codes = round256((size_t)M * p.blocks * 16);
