@@ -445,3 +445,45 @@ def test_gradients_of_rows_far_apart(ld, m):
     lp.lp_ckpt8_fc_wgrad(m, k, n, d, x[0], x[1], dw, workspace=workspace(lp.lp_ckpt8_fc_wgrad_workspace_bytes(m, k, n)))
     want, size = product(dy.cuda().t(), x[2])
     mx.close(dw, want, mx.product_error(size, m), torch.float32)
+
+
+def anywhere(t, fill, start, gap):
+    """t in memory that begins `start` elements into a buffer of `fill`, its rows `gap` elements apart."""
+    m, n = t.shape
+    buffer = torch.full((start + m * (n + gap) + 8,), fill, dtype=t.dtype, device="cuda")
+    view = buffer.as_strided((m, n), (n + gap, 1), start)
+    view.copy_(t)
+    return view, buffer
+
+
+def around_is_left(buffer, view, fill):
+    view.fill_(fill)
+    assert torch.equal(buffer, torch.full_like(buffer, fill))
+
+
+@pytest.mark.parametrize("size", [(3, 300, 7), (70, 129, 65), (130, 257, 192), (257, 500, 129)])
+@pytest.mark.parametrize("start, gap", [(1, 0), (1, 1), (3, 2), (2, 17)])
+def test_tensors_that_begin_anywhere(size, start, gap):
+    m, k, n = size
+    nan = float("nan")
+    w = weights(n, k, 1)
+    x = inputs(m, k, torch.float16, 2)
+    xd, _ = anywhere(x, nan, start, gap)
+    y, buffer = anywhere(torch.zeros((m, n), dtype=torch.bfloat16), 5.0, start, gap)
+    run_fwd(m, k, n, xd, w, y)
+    want, sums = product(torch.from_numpy(mx.mx4_values(*mx.mx4_quantize(x.double().numpy())[:2], k)).cuda(), w[2].t())
+    mx.close(y, want, mx.product_error(sums, k), torch.bfloat16)
+    around_is_left(buffer, y, 5.0)
+    dy = inputs(m, n, torch.bfloat16, 3)
+    d, _ = anywhere(dy, nan, start, gap)
+    dx, buffer = anywhere(torch.zeros((m, k)), 5.0, start, gap)
+    lp.lp_mx4_fc_dgrad(m, k, n, d, w[0], w[1], dx, workspace=workspace(lp.lp_mx4_fc_dgrad_workspace_bytes(m, k, n)))
+    want, sums = product(dy.cuda(), w[2])
+    mx.close(dx, want, mx.product_error(sums, n), torch.float32)
+    around_is_left(buffer, dx, 5.0)
+    kept_x = kept(m, k, 4)
+    dw, buffer = anywhere(torch.zeros((n, k), dtype=torch.bfloat16), 5.0, start, gap)
+    lp.lp_ckpt8_fc_wgrad(m, k, n, d, kept_x[0], kept_x[1], dw, workspace=workspace(lp.lp_ckpt8_fc_wgrad_workspace_bytes(m, k, n)))
+    want, sums = product(dy.cuda().t(), kept_x[2])
+    mx.close(dw, want, mx.product_error(sums, m), torch.bfloat16)
+    around_is_left(buffer, dw, 5.0)
