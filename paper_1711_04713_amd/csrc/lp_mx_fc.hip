@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "lp_mx.h"
+#include "lp_mx_tile.h"
 
 namespace lp {
 
@@ -563,10 +564,10 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
 {
     constexpr int TI = MB * 32 * WM, TJ = NB * 32 * WN, WAVES = WM * WN, THREADS = WAVES * 64;
     constexpr int ABYTES = TI * 128, BBYTES = TJ * 128, STAGE = ABYTES + BBYTES;
-    constexpr int PER = ABYTES / 1024 / WAVES; // a wave's loads of dY per stage, and a thread's pieces
-    constexpr int AROW = WEIGHTS ? TI * 2 : 128, BROW = TJ * 2;
-    constexpr int ATURN = (AROW < 256 ? AROW / 64 : 4) - 1, BTURN = (BROW < 256 ? BROW / 64 : 4) - 1; // 64-byte pieces that change places
-    static_assert((AROW & (AROW - 1)) == 0 && (BROW & (BROW - 1)) == 0, "places are exchanged within a row");
+    typedef DyTile<TI, WAVES, WEIGHTS> Dy;
+    constexpr int PER = Dy::PER, AROW = Dy::ROW, ATURN = Dy::TURN, BROW = TJ * 2;
+    constexpr int BTURN = (BROW < 256 ? BROW / 64 : 4) - 1; // 64-byte pieces that change places
+    static_assert((BROW & (BROW - 1)) == 0, "places are exchanged within a row");
     static_assert(TJ * 2 == THREADS, "a thread decodes one block of 32 per stage");
     __shared__ __align__(1024) unsigned char lds[2 * STAGE];
     static_assert(WAVES * result_bytes(NB) <= (int)sizeof(lds), "results pass through the same memory");
@@ -583,21 +584,13 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
     // further than into the next row.)
     const bool direct = WORDS || (a.ld < kNearRows && (!WEIGHTS || a.ld >= 8));
     const int whole = direct ? last - ragged : first;
+    // row and piece of the row that this lane brings, and where in a stage's buffer
+    auto dy_row = [&](int q) __attribute__((always_inline)) { return Dy::row(Dy::number(wave, q, lane)); };
+    auto dy_piece = [&](int q) __attribute__((always_inline)) { return Dy::piece(Dy::number(wave, q, lane)); };
+    auto dy_place = [&](int buf, int q) __attribute__((always_inline)) { return lds + buf * STAGE + Dy::number(wave, q, lane) * 16; };
     unsigned at[PER];
 #pragma unroll
-    for (int q = 0; q < PER; ++q) {
-        if constexpr (!WORDS) {
-            const int k = q * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
-            at[q] = (unsigned)(WEIGHTS ? r : min(r, a.I - 1 - i0)) * (unsigned)(a.ld * 2) + s * 16;
-        } else if constexpr (WEIGHTS) {
-            constexpr int LANES = AROW / 16; // of a row
-            const int r = (wave * PER + q) * (64 / LANES) + lane / LANES, s = lane % LANES;
-            at[q] = (unsigned)r * (unsigned)(a.ld * 2) + (((s >> 2) ^ (r & ATURN)) * 4 + (s & 3)) * 16;
-        } else {
-            const int r = (wave * PER + q) * 8 + lane / 8;
-            at[q] = (unsigned)min(r, a.I - 1 - i0) * (unsigned)(a.ld * 2) + ((lane & 7) ^ (r & 7)) * 16;
-        }
-    }
+    for (int q = 0; q < PER; ++q) at[q] = (unsigned)(WEIGHTS ? dy_row(q) : min(dy_row(q), a.I - 1 - i0)) * (unsigned)(a.ld * 2) + dy_piece(q) * 16;
     // loads FROM .. TO - 1 of a wave's share of stage t; where nothing is to come the descriptor is empty and zeros arrive
     auto load_dy = [&](int t, int buf, auto from, auto to) __attribute__((always_inline)) {
         if constexpr (WORDS) {
@@ -609,7 +602,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
             const int size = __builtin_amdgcn_readfirstlane(t < whole ? all : 0);
             const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<__bf16 *>(base), 0, size, 0x00020000);
 #pragma unroll
-            for (int q = decltype(from)::value; q < decltype(to)::value; ++q) load_lds16(rsrc, lds + buf * STAGE + (wave * PER + q) * 1024, at[q], 0);
+            for (int q = decltype(from)::value; q < decltype(to)::value; ++q) load_lds16(rsrc, lds + buf * STAGE + Dy::number(wave, q, 0) * 16, at[q], 0);
         }
     };
     // A thread's pieces of a stage at once, or in two halves where registers are short beside a large tile's sums.  (8192 x 4096
@@ -629,6 +622,8 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
         }
     };
     // A stage at once, the ragged one for instance: as many pieces on their way together as there are registers for beside the sums.
+    // (Where dY comes by loads to LDS, empty ones of this stage left zeros in the pieces that are written here.  They are this
+    // wave's own, and it has waited for them; other waves' may still be on their way.)
     auto bring_dy = [&](int t, int buf) __attribute__((always_inline)) {
         constexpr int TOGETHER = MB * NB >= 8 ? 1 : PER;
         const int rows = WEIGHTS ? a.C : a.I, cols = WEIGHTS ? a.I : a.C;
@@ -637,27 +632,19 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
             v4u piece[TOGETHER];
 #pragma unroll
             for (int q = 0; q < TOGETHER; ++q) {
-                const int k = (q0 + q) * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
+                const int r = dy_row(q0 + q), s = dy_piece(q0 + q);
                 const int row = WEIGHTS ? t * 64 + r : i0 + r, col = WEIGHTS ? i0 + s * 8 : t * 64 + s * 8;
                 if (rows < 1 || cols < 8) piece[q] = load_piece(a.dy + row * a.ld + col, row < rows ? cols - col : 0);
                 else piece[q] = load_tail(a.dy + min(row, rows - 1) * a.ld, row < rows ? col : cols, cols);
             }
-            __builtin_amdgcn_s_waitcnt(0); // (and the zeros of the empty loads have arrived)
+            __builtin_amdgcn_s_waitcnt(0); // (and the zeros of this wave's empty loads have arrived)
 #pragma unroll
-            for (int q = 0; q < TOGETHER; ++q) {
-                const int k = (q0 + q) * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
-                const int to = WEIGHTS ? ((s >> 2) ^ (r & ATURN)) * 4 + (s & 3) : s ^ (r & 7);
-                *(v4u *)(lds + buf * STAGE + r * AROW + to * 16) = piece[q];
-            }
+            for (int q = 0; q < TOGETHER; ++q) *(v4u *)dy_place(buf, q0 + q) = piece[q];
         }
     };
     auto place_dy = [&](int buf, int half) __attribute__((always_inline)) {
 #pragma unroll
-        for (int q = 0; q < HALF; ++q) {
-            const int k = (half * HALF + q) * THREADS + threadIdx.x, r = k / (AROW / 16), s = k % (AROW / 16);
-            const int to = WEIGHTS ? ((s >> 2) ^ (r & ATURN)) * 4 + (s & 3) : s ^ (r & 7);
-            *(v4u *)(lds + buf * STAGE + r * AROW + to * 16) = raw_dy[q];
-        }
+        for (int q = 0; q < HALF; ++q) *(v4u *)dy_place(buf, half * HALF + q) = raw_dy[q];
     };
 
     // B: thread's row of the stage and block of the row.  The descriptors start at a stage's first row and end with the tensor.
