@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void ckpt8_save_kernel(const T *x, size_t
     codes[p] = w;
     if ((p & 3) == 0) scales[p >> 2] = (unsigned char)e;
     if (y) {
-        store8(y + row * ldy + col, n, act_values(v, act));
+        store8(y + row * ldy + col, n, act_values<T>(v, act));
     }
 }
 
@@ -198,10 +198,7 @@ __global__ __launch_bounds__(kThreads) void ckpt8_act_bwd_kernel(const v2u *__re
     if (col >= g.cols) return;
     const int n = (int)min(g.cols - col, 8u);
     const v8f h = ckpt8_values(codes[p], scales[p >> 2]);
-    v8f d = load8(dy + row * lddy + col, n);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) d[j] *= act_slope(h[j], act);
-    store8(dx + row * lddx + col, n, d);
+    store8(dx + row * lddx + col, n, act_gradients<T>(load8(dy + row * lddy + col, n), h, act));
 }
 
 // ---------------------------------------------------------------------------------- launches

@@ -54,7 +54,7 @@ __device__ __forceinline__ void put(const Sink &s, T *to, const float *bias, int
 {
     if (s.bias) v += load_floats<W>(bias, n);
     if (s.accumulate) v += load_floats<W>(to, n);
-    store_floats<W>(to, n, act_values(v, s.act));
+    store_floats<W>(to, n, act_values<T>(v, s.act));
 }
 
 // A wave's results, MB x NB blocks of 32 rows x 32 columns from (i0, j0) of a tile on, of which I x J exist: 32 rows at a time
