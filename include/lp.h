@@ -331,8 +331,8 @@ lp_status lp_maxpool2x2(const void *x_codes_dev, void *y_codes_dev, int N, int H
  * value in 32 bits): mx4 e = E - 2, kept within 2..252 (the usual rule of this format: the largest value
  * lies in [4, 8) and saturates above 6); ckpt8 e = E, kept within 7..254 (the largest lies in [64, 128)).
  * Every value of either format is a normal number of 32 bits or zero, so smaller magnitudes round to zero.
- * As in lp_quantize NaN becomes 0 and what does not fit saturates, infinities included.  The sign of
- * zero is kept by mx4.
+ * As in lp_quantize NaN becomes 0 and what does not fit saturates, infinities included.  mx4 codes have the
+ * sign of the value, also where this is a zero or rounds to one.
  *
  * Float tensors (x, y, dy, dx, dw) are row-major with their own row stride ld >= columns, in elements; they
  * and the bias need the alignment of their type only.  Codes are aligned to 16 bytes, mx4 scales to 8, ckpt8

@@ -101,7 +101,7 @@ __global__ __launch_bounds__(COUNT ? kCountThreads : kThreads) void mx4_quantize
             for (int j = 0; j < 8; ++j) {
                 const float a = v[j] == v[j] ? v[j] : 0.0f;
                 const int c = mx4_code<MODE>(fabsf(a) * inv, draw[j]);
-                w |= (unsigned)(min(c, 7) | (a < 0.0f ? 8 : 0)) << (4 * j);
+                w |= ((unsigned)min(c, 7) | (__float_as_uint(a) >> 28 & 8)) << (4 * j); // (-0 too)
                 if (COUNT) {
                     zeros += j < n && c == 0;
                     sats += j < n && c > 7;
