@@ -335,7 +335,7 @@ lp_status lp_maxpool2x2(const void *x_codes_dev, void *y_codes_dev, int N, int H
  * sign of the value, also where this is a zero or rounds to one.
  *
  * Float tensors (x, y, dy, dx, dw) are row-major with their own row stride ld >= columns, in elements; they
- * and the bias need the alignment of their type only.  Codes are aligned to 16 bytes, mx4 scales to 8, ckpt8
+ * and the bias need the alignment of their type only.  Codes are aligned to 16 bytes, mx4 scales and counters to 8, ckpt8
  * scales not at all.  What lies between a row's last column and the next row is neither used nor written.  No tensor may
  * overlap another one of the call unless its text says so.  Calls without rows do
  * nothing and return LP_OK.

@@ -364,10 +364,14 @@ def _refuse(what, why):
 
 # What the C entry points cannot see for themselves: where the tensors are, their own sizes and strides.
 
-def _here(t, device, what, name):
-    """Address of a tensor that has to be on the current GPU, whose stream the call goes to (None: a null pointer)."""
+# Tensors have to be on the current GPU, whose stream the call goes to.
+
+def _counter(t, device, what, name):
+    """Address of an integer of 64 bits, the tensor's first (None: a null pointer)."""
     if t is None:
         return None
+    if t.element_size() != 8 or t.is_floating_point() or t.is_complex() or not t.numel():
+        _refuse(what, "%s is not an integer of 64 bits" % name)
     if t.get_device() != device:
         _refuse(what, "%s is not on the current GPU" % name)
     return t.data_ptr()
@@ -420,7 +424,7 @@ def _vector(t, n, device, what, name):
 
 def _workspace(t, device, what):
     """Address and bytes of a workspace."""
-    return (None, 0) if t is None else (_here(t, device, what, "workspace"), t.nbytes)
+    return (None, 0) if t is None else (_dense(t, t.nbytes, device, what, "workspace"), t.nbytes)
 
 
 def _bf16(t, what, name):
@@ -456,8 +460,8 @@ def lp_mx4_quantize(x, codes, scales, r=LP_ROUND_NEAREST_EVEN, seed=0, zero_coun
     rows, cols = x.shape
     px, ldx = _rows(x, rows, cols, device, what, "x")
     pc, ps = _mx4(codes, scales, rows, cols, device, what, "x")
-    _check(load().lp_mx4_quantize(px, _dtype(x), rows, cols, ldx, pc, ps, r, seed, _here(zero_count, device, what, "zero_count"),
-                                  _here(sat_count, device, what, "sat_count"), _stream()), what)
+    pz, psat = _counter(zero_count, device, what, "zero_count"), _counter(sat_count, device, what, "sat_count")
+    _check(load().lp_mx4_quantize(px, _dtype(x), rows, cols, ldx, pc, ps, r, seed, pz, psat, _stream()), what)
 
 
 def lp_mx4_dequantize(codes, scales, y):

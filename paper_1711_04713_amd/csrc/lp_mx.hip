@@ -273,6 +273,7 @@ extern "C" lp_status lp_mx4_quantize(const void *x_dev, lp_dtype xt, size_t rows
     if (!dtype_ok(xt) || (int)r < 0 || (int)r > 2) return LP_EINVAL;
     if (rows == 0 || cols == 0) return LP_OK;
     if (!floats_ok(x_dev, xt, cols, ldx) || !codes_dev || !aligned16(codes_dev) || !scales_dev || !aligned_to(scales_dev, 8)) return LP_EINVAL;
+    if (!aligned_to(zero_count_dev, 8) || !aligned_to(sat_count_dev, 8)) return LP_EINVAL;
     PieceGrid g;
     if (!piece_grid(rows, cols, mx4_blocks(cols), &g)) return LP_EUNSUPPORTED;
     hipStream_t st = as_stream(stream);
