@@ -398,7 +398,10 @@ lp_status lp_mx4_fc_dgrad(int M, int K, int Nout, const void *dy_dev, size_t ldd
  * y = act(x) (same type as x, row stride ldy; y_dev may be x_dev if ldy == ldx) in the same pass.  r as in lp_quantize.
  * lp_ckpt8_load -- the kept values, rounded to yt (nearest even).
  * lp_ckpt8_act_bwd -- dx = dy * act'(kept value); dy and dx of type t, dx_dev may be dy_dev if the strides are equal.
- * At 0 the slope of LP_ACT_RELU is 0.  LP_EUNSUPPORTED as lp_mx4_quantize.
+ * At 0 the slope of LP_ACT_RELU is 0, and what is kept as 0 counts as 0: the gradient of a positive value below 1/128 to 1/256 of
+ * its block's largest magnitude (nearest rounding) is dropped though its y was not.  Of normally distributed values these are 1.1 % of the
+ * positive ones, 6 to 7 % where neighbours differ by an order of magnitude; a caller that cannot spare them masks dy by y > 0 instead.
+ * LP_EUNSUPPORTED as lp_mx4_quantize.
  */
 lp_status lp_ckpt8_save(const void *x_dev, lp_dtype xt, size_t rows, size_t cols, size_t ldx, void *codes_dev,
                         void *scales_dev, lp_round r, uint64_t seed, lp_actfn act, void *y_dev, size_t ldy,

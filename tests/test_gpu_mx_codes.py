@@ -67,3 +67,19 @@ def test_numbers_below_the_normal_ones(dtype, mode):
     lp.lp_ckpt8_save(x.cuda(), codes, scales, r=ROUNDINGS[mode], seed=seed)
     assert np.array_equal(scales.cpu().numpy(), want[1])
     assert np.array_equal(codes.cpu().numpy(), want[0])
+
+
+def test_relu_gradient_of_values_that_are_kept_as_zero():
+    """The slope is that of the kept value: half a step of the block (2^-5 here) and less is 0, a little more is not."""
+    x = torch.zeros((1, 64))
+    x[0, 0], x[0, 1:7] = 4.0, torch.tensor([2.0 ** -5, 2.0 ** -5 * 1.01, 2.0 ** -9, -1.0, 1.0, -(2.0 ** -5) * 1.01])
+    x[0, 32:40] = torch.tensor([2.0 ** -5, 2.0 ** -7, 2.0 ** -9, 2.0 ** -13, 2.0 ** -12 * 1.01, -0.0, 0.0, -1e-9])    # largest: 2^-5
+    codes, scales = ckpt8_buffers(1, 64)
+    y, dx = torch.empty((1, 64), device="cuda"), torch.empty((1, 64), device="cuda")
+    lp.lp_ckpt8_save(x.cuda(), codes, scales, act=lp.LP_ACT_RELU, y=y)
+    lp.lp_ckpt8_act_bwd(codes, scales, torch.full((1, 64), 3.0, device="cuda"), dx, lp.LP_ACT_RELU)
+    want = torch.zeros((1, 64))
+    want[0, [0, 2, 5]] = 3.0
+    want[0, [32, 33, 34, 36]] = 3.0
+    assert torch.equal(dx.cpu(), want)
+    assert torch.equal(y.cpu() > 0, x > 0)
