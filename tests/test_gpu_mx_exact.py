@@ -76,3 +76,37 @@ def test_weight_gradient_of_ragged_reductions_and_tiles(size, extra):
         lp.lp_ckpt8_fc_wgrad(m, k, n, d, codes, scales, dw, dbias=db, workspace=ws)
         assert torch.equal(dw, want.to(dtype))
         assert torch.equal(db, sums.float())
+
+
+def mx4_of_blocks(rows, cols, seed, spread):
+    """mx4 with a 6 in every block, so that its floats are quantized back to it, and scales of 2^-spread .. 2^spread; values."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    codes, scales, values = mx4(rows, cols, seed)
+    codes[:, ::16] = codes[:, ::16] & 0xF0 | 7
+    values[:, ::32] = 6.0
+    codes[:, (cols + 31) // 32 * 16:] = 0
+    if spread:
+        scales += torch.randint(-spread, spread + 1, scales.shape, generator=g, device="cuda").to(torch.uint8)       # (wraps round)
+        values *= torch.exp2(scales.double() - 127).repeat_interleave(32, 1)[:, :cols]
+    return codes, scales, values
+
+
+# few rows, tiles of 64, 128 and 256 rows, parts, cut last rounds, reductions of one stage of 256 to 98 and any remainder; sums below
+# 36 K in steps of 1/4, with scales 144 K in steps of 1/16: below 2^24 of them
+@pytest.mark.parametrize("size", [(1, 4096, 640), (3, 25088, 65), (16, 1500, 300), (16, 25088, 256), (20, 25088, 4096), (40, 25088, 300), (64, 4096, 4096),
+                                  (256, 25088, 4096), (600, 25088, 1000), (130, 255, 190), (700, 257, 700), (1030, 4000, 4100), (2048, 4096, 2050),
+                                  (4328, 2048, 197), (4100, 4096, 4100), (4090, 4096, 8200), (4000, 8100, 4090)])
+def test_forward_of_deep_and_ragged_products(size):
+    m, k, n = size
+    spread = 1 if k <= 4096 else 0
+    x, w = mx4_of_blocks(m, k, 5, spread), mx4_of_blocks(n, k, 6, spread)
+    want = torch.mm(x[2], w[2].t().contiguous())
+    ws = workspace(lp.lp_mx4_fc_workspace_bytes(m, k, n))
+    for dtype in (torch.float32, torch.bfloat16):
+        for codes in (True, False):
+            y = torch.full((m, n), float("nan"), dtype=dtype, device="cuda")
+            if codes:
+                lp.lp_mx4_fc_fwd(m, k, n, x[0], w[0], w[1], y, x_scales=x[1], workspace=ws)
+            else:
+                lp.lp_mx4_fc_fwd(m, k, n, x[2].to(dtype), w[0], w[1], y, workspace=ws)                                # (exact in both types)
+            assert torch.equal(y, want.to(dtype))
