@@ -432,14 +432,27 @@ def _bf16(t, what, name):
         _refuse(what, "%s is not bfloat16" % name)
 
 
+# Sizes as the C calls take them.  One that their type does not hold becomes its largest number, which every call refuses: ctypes
+# would cut it off.
+
+def _ints(*sizes):
+    return tuple(min(max(n, -1), 0x7fffffff) for n in sizes)
+
+
+def _size(n):
+    return n if 0 <= n < 1 << 64 else (1 << 64) - 1
+
+
 def _two_sizes(what, rows, cols):
     a, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
-    _check(getattr(load(), what)(rows, cols, ctypes.byref(a), ctypes.byref(b)), what)
+    _check(getattr(load(), what)(_size(rows), _size(cols), ctypes.byref(a), ctypes.byref(b)), what)
     return a.value, b.value
 
 
 def _fc_workspace_bytes(what, M, K, Nout):
     n = ctypes.c_size_t(0)
+    if (M | K | Nout) >> 31:
+        M, K, Nout = _ints(M, K, Nout)
     _check(getattr(load(), what)(M, K, Nout, ctypes.byref(n)), what)
     return n.value
 
@@ -487,6 +500,8 @@ def lp_mx4_fc_fwd(M, K, Nout, x, w_codes, w_scales, y, x_scales=None, bias=None,
     pc, ps = _mx4(w_codes, w_scales, Nout, K, device, what, "w")
     pb = _vector(bias, Nout, device, what, "bias")
     pw, nw = _workspace(workspace, device, what)
+    if (M | K | Nout) >> 31:
+        M, K, Nout = _ints(M, K, Nout)
     _check(load().lp_mx4_fc_fwd(M, K, Nout, px, xt, ldx, pxs, pc, ps, pb, py, _dtype(y), ldy, act, pw, nw, _stream()), what)
 
 
@@ -502,6 +517,8 @@ def lp_mx4_fc_dgrad(M, K, Nout, dy, w_codes, w_scales, dx, workspace=None):
     pdx, lddx = _rows(dx, M, K, device, what, "dx")
     pc, ps = _mx4(w_codes, w_scales, Nout, K, device, what, "w")
     pw, nw = _workspace(workspace, device, what)
+    if (M | K | Nout) >> 31:
+        M, K, Nout = _ints(M, K, Nout)
     _check(load().lp_mx4_fc_dgrad(M, K, Nout, pdy, lddy, pc, ps, pdx, _dtype(dx), lddx, pw, nw, _stream()), what)
 
 
@@ -552,4 +569,6 @@ def lp_ckpt8_fc_wgrad(M, K, Nout, dy, x_codes, x_scales, dw, dbias=None, accumul
     pc, ps = _ckpt8(x_codes, x_scales, M, K, device, what, "x")
     pb = _vector(dbias, Nout, device, what, "dbias")
     pw, nw = _workspace(workspace, device, what)
+    if (M | K | Nout) >> 31:
+        M, K, Nout = _ints(M, K, Nout)
     _check(load().lp_ckpt8_fc_wgrad(M, K, Nout, pdy, lddy, pc, ps, pdw, _dtype(dw), lddw, pb, int(bool(accumulate)), pw, nw, _stream()), what)

@@ -56,3 +56,47 @@ def test_workspaces_are_dense(on_the_cpu):
         for bad in (torch.zeros((4096, 2))[:, 0], torch.zeros(1, dtype=torch.uint8).expand(4096), torch.zeros((8, 8)).t()[1:]):
             with pytest.raises(ValueError):
                 call(bad)
+
+
+EUNSUPPORTED = 2
+LONG = (1 << 32) + 4      # rows that an int of 32 bits holds as 4
+
+
+def test_sizes_that_an_int_does_not_hold_are_refused():
+    for f in (lp.lp_mx4_fc_workspace_bytes, lp.lp_mx4_fc_dgrad_workspace_bytes, lp.lp_ckpt8_fc_wgrad_workspace_bytes):
+        for dims in ((LONG, 40, 24), (4, LONG, 24), (4, 40, LONG), (1 << 64, 40, 24)):
+            with pytest.raises(lp.LpError) as e:
+                f(*dims)
+            assert e.value.status == EUNSUPPORTED
+        for dims in ((-LONG, 40, 24), (-(1 << 33) + 4, 40, 24), (4, -(1 << 32) + 40, 24)):
+            with pytest.raises(lp.LpError) as e:
+                f(*dims)
+            assert e.value.status == EINVAL
+    for f in (lp.lp_mx4_bytes, lp.lp_ckpt8_bytes):
+        for dims in (((1 << 64) + 4, 40), (4, (1 << 64) + 40), (-(1 << 64) + 4, 40), (-4, 40)):
+            with pytest.raises(lp.LpError) as e:
+                f(*dims)
+            assert e.value.status == EUNSUPPORTED
+
+
+def test_products_of_more_rows_than_an_int_holds_are_refused(monkeypatch, on_the_cpu):
+    """Tensors without memory (the calls return before they would follow an address)."""
+    seen = []
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: seen.append((name, args)) or 0
+
+    monkeypatch.setattr(binding, "load", Library)
+    monkeypatch.setattr(binding, "_stream", lambda: None)
+
+    def meta(rows, cols, dtype=torch.bfloat16):
+        return torch.empty((rows, cols), dtype=dtype, device="meta")
+
+    monkeypatch.setattr(binding, "_device", lambda: meta(1, 1).get_device())
+    w = meta(1, 128, torch.uint8), meta(1, 8, torch.uint8)
+    lp.lp_mx4_fc_fwd(LONG, 1, 1, meta(LONG, 1), *w, meta(LONG, 1))
+    lp.lp_mx4_fc_dgrad(LONG, 1, 1, meta(LONG, 1), *w, meta(LONG, 1))
+    lp.lp_ckpt8_fc_wgrad(LONG, 1, 1, meta(LONG, 1), meta(LONG, 32, torch.int8), meta(LONG, 1, torch.uint8), meta(1, 1))
+    assert [name for name, _ in seen] == ["lp_mx4_fc_fwd", "lp_mx4_fc_dgrad", "lp_ckpt8_fc_wgrad"]
+    assert all(1 << 24 < args[0] < 1 << 31 and args[1:3] == (1, 1) for _, args in seen)        # above the calls' limit, and held by an int
