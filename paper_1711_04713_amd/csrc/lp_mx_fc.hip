@@ -823,10 +823,10 @@ static double stage_cost(const TileCost &c, long long work)
 constexpr TileCost kMx4Tiles[4] = {{64, 64, 0.175, 0.2, 1.9, 0.8}, {128, 128, 0.345, 0.51, 3.35, 2.85}, {256, 256, 1.03, 1.58, 4.9, 3.2}, {128, 128, 0.54, 0.49, 2.6, 1.35}};
 // 64 x 128, 128 x 128, 256 x 256; a stage is 64 positions
 constexpr TileCost kInputTiles[3] = {{64, 128, 0.39, 0.315, 2.65, 0.45}, {128, 128, 0.505, 0.455, 3.15, 0.0}, {256, 256, 1.19, 1.34, 4.1, 0.0}};
-constexpr TileCost kWeightTiles[3] = {{64, 128, 0.91, 0.405, 4.75, 0.65}, {128, 128, 0.77, 0.535, 4.95, 1.75}, {256, 256, 1.265, 1.51, 8.5, 6.1}};
-// The same where Nout is odd: every other row of a dense dY starts inside a word, and all of it goes through registers.  (By the
-// other table: 601 x 768 over 256 rows 12.6 us instead of 8.9, 4097 x 4096 over 4096 248 instead of 200.)
-constexpr TileCost kOddWeightTiles[3] = {{64, 128, 0.715, 0.485, 3.75, 0.45}, {128, 128, 1.1, 0.675, 5.1, 1.25}, {256, 256, 1.64, 1.57, 8.0, 3.05}};
+// The weights' gradient, whichever way dY comes to LDS: the timings of both ways are fitted together, so that the choice depends on
+// the sizes alone.  (With a table for each, chosen by the parity of Nout, a dY whose stride had the other parity got the other's
+// tile, and 600 x 768 over 256 rows took 9.4 us instead of 7.2.)
+constexpr TileCost kWeightTiles[3] = {{64, 128, 0.59, 0.42, 3.85, 0.565}, {128, 128, 0.825, 0.56, 4.68, 1.455}, {256, 256, 1.3, 1.605, 8.265, 3.825}};
 
 // How a product I x J with `stages` stages of its reduction is cut into workgroups.
 struct Cut {
@@ -836,9 +836,10 @@ struct Cut {
     double us;
 };
 
-// The cheapest of the tiles and numbers of parts, by an estimate that the tables above were fitted to (2373 timings of 324
-// problems: the choice costs 1.2 % on the average; it is a part too many or too few, 10 to 30 % of 5 to 15 us, where it is
-// worst).  Results leave at 44 GB/s a compute unit; joining the parts is a launch, and their sums go through memory at
+// The cheapest of the tiles and numbers of parts, by an estimate that the tables above were fitted to (2915 timings of 380
+// problems with operands in the caches: against the best of each the choice costs 0.2 % of a forward product on the average, 1 to 1.6 %
+// of a gradient; it is a part too many or too few, 10 to 25 %, where it is worst).  What operands take that come from
+// memory is not in it.  Results leave at 44 GB/s a compute unit; joining the parts is a launch, and their sums go through memory at
 // 7.5 TB/s.  A part has `step` stages or a multiple of them, and `least` at least.
 template <int SIZES>
 static Cut cut_product(int I, int J, int stages, int step, int least, const TileCost (&tiles)[SIZES], int out_bytes)
@@ -957,7 +958,7 @@ static void few_launch(const Mx4Args &a, const void *x, lp_dtype xt, size_t ldx,
 
 static Cut grad_cut(int I, int J, int C, bool weights)
 {
-    return cut_product(I, J, std::max((C + 63) / 64, 1), 1, 4, !weights ? kInputTiles : I % 2 ? kOddWeightTiles : kWeightTiles, 4);
+    return cut_product(I, J, std::max((C + 63) / 64, 1), 1, 4, weights ? kWeightTiles : kInputTiles, 4);
 }
 
 template <bool WEIGHTS, typename T>
