@@ -212,10 +212,11 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const Grid g, Sink out,
 //
 // Weights are the row operand: a lane ends up with four neighbouring columns of one row of y.
 //
-// Measured with codes in hand: 8192 x 14336 from 4096 245 to 260 us, 3.7 to 3.9 PFLOP/s (x in bfloat16: 345 to 360 with its
-// quantization and in a long run, where the clock falls to 1.3 GHz: the chip's power, not its pipes, bounds the large tiles); 256 x 4096 from
-// 25088 28.8 us, 64 x 4096 from 4096 7.2: tiles of 64 rows are bound by their loads (0.2 us for 16 KB a stage and unit) and,
-// alone on a unit, by the chain of a stage's barrier, reads and products.
+// Measured with codes in hand: 8192 x 14336 from 4096 250 to 260 us, 3.7 to 3.85 PFLOP/s (with SiLU 265 to 300).
+// Its clock is 1.57 GHz and a stage 3030 cycles, 2048 of them the products'; with loads that
+// touch no memory 1.89 GHz and 2870 cycles: what bounds the large tiles is first the clock under this load.  256 x 4096 from 25088 26 to
+// 28 us (39 where the weights come from memory), 64 x 4096 from 4096 6.0: tiles of 64 rows are bound by their loads (0.2 us for 16 KB a stage and unit) and,
+// alone on a unit, by the chain of a stage's barrier, reads and products: 540 cycles a stage, 480 with loads that touch no memory.
 struct Mx4Args {
     const unsigned char *xc, *xs, *wc, *ws;
     int M, N, K, blocks;
@@ -455,7 +456,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void mx4_few_kernel(const Mx4Arg
 // A workgroup owns TI x TJ results, a wave MB x NB blocks of 32 x 32; a stage is 64 positions of the reduction in one of two
 // LDS buffers.  B's codes pass through registers, a block of 32 a thread, and are decoded one stage ahead; dY
 // comes by loads to LDS (or, where its rows do not start on words, through registers like the codes: 200 x 4096 from 1001
-// columns 13.0 us, from 1002 12.5; 8192 x 4096 from 14337 1020, from 14338 750).  The matrix
+// columns 11.5 us, from 1002 10.9; 8192 x 4096 from 14337 880 to 925, from 14338 740 to 785).  The matrix
 // instruction wants eight neighbouring positions of a row or column in a lane: those of dY's rows lie together in memory
 // (16-byte piece p of row r at place p ^ (r % 8), as above); tiles with the reduction along their rows are read by
 // ds_read_b64_tr_b16, which hands each of 16 lanes four rows' elements of its column.  Their rows are 512 (or 256) bytes, so
@@ -464,9 +465,10 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void mx4_few_kernel(const Mx4Arg
 //
 // B is the row operand of the instruction, so that a lane ends up with four neighbouring columns of one row of D.
 //
-// Measured: 8192 x 4096 from 14336 730 to 760 us, 1.27 to 1.32 PFLOP/s; weights 14336 x 4096 over 8192 845 to 870, 1.11 to
-// 1.14 (a library product of two bfloat16 tensors of these sizes reaches 1.2 to 1.5).  A stage of the large tile takes 3170 cycles at
-// 1.7 GHz, 2384 without the decoding (2048 are the products'); 256 x 4096 weights over 256 rows 22 us: 16.8 MB leave at 3 TB/s.
+// Measured: 8192 x 4096 from 14336 715 to 760 us, 1.27 to 1.34 PFLOP/s; weights 14336 x 4096 over 8192 850 to 900, 1.07 to
+// 1.13 (a library product of two bfloat16 tensors of these sizes reaches 1.2 to 1.5).  A stage of the large tile takes 2890 cycles (2048 are
+// the products') at 1.85 GHz; with codes that are not decoded 2880 at 2.02, 680 us: the decoding costs clock, not cycles.  Weights 3270
+// at 1.87, 3000 at 2.01 and 750 us.  256 x 4096 weights over 256 rows 21 us: 16.8 MB leave at 3 TB/s.
 struct GradArgs {
     const __bf16 *dy;
     size_t ld;
@@ -606,7 +608,7 @@ __global__ __launch_bounds__(WM *WN * 64, 2) void gradient_kernel(const GradArgs
         }
     };
     // A thread's pieces of a stage at once, or in two halves where registers are short beside a large tile's sums.  (8192 x 4096
-    // from 14337: 1.21 ms at once, 1.02 in halves; weights 14337 x 4096 over 8192: 0.99, 1.04.)
+    // from 14337: 1.10 ms at once, 0.92 in halves; weights 14337 x 4096 over 8192 the same in both.)
     constexpr int HALF = MB * NB >= 8 && !WEIGHTS ? PER / 2 : PER;
     v4u raw_dy[HALF] = {};
     auto fetch_dy = [&](int t, int half) __attribute__((always_inline)) {
@@ -913,7 +915,9 @@ static Mx4Plan mx4_plan(int M, int K, int Nout)
     if (M <= 16) {
         // Few rows: every workgroup reads 16 rows of w and all of x, 8 TB/s in all, a wave's chunk takes half a microsecond.
         // Quantizing x is a launch of 2.3 us, or 0.35 us a row and chunk where every wave does it.
-        // us, few rows : tiles, bf16: 1 x 4096 -> 4096 4.1 : 8.6, 16 rows 7.2 : 8.6, 16 x 4096 -> 14336 13.5 : 8.8
+        // us, few rows : tiles, bf16: 1 x 4096 -> 14336 9.0 : 9.9, 16 rows 15.7 : 10.7, 1 x 14336 -> 4096 8.3 : 13.3, 8 rows 12.8 : 13.8.
+        // (The rate is the caches'.  Weights that come from memory take longer in either, which leaves the choice as it is: with ten
+        // layers' in turn 9.7 : 10.7, 17.8 : 11.5, 9.2 : 14.2, 13.3 : 14.8; 1 x 4096 -> 131072, 285 MB, 50.7 : 49.8.)
         const double chunks = (double)((p.blocks + 16 * kFewWaves - 1) / (16 * kFewWaves));
         const double read = (double)Nout * p.blocks * 17 * (1 + M / 16.0) / 8e6;
         few_floats = 0.35 * M * chunks;
