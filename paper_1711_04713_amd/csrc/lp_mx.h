@@ -17,6 +17,17 @@ inline size_t dtype_size(lp_dtype t) { return t == LP_F32 ? 4 : 2; }
 inline bool dtype_ok(lp_dtype t) { return (int)t >= 0 && (int)t <= 2; }
 inline bool actfn_ok(lp_actfn f) { return (int)f >= 0 && (int)f <= 3; }
 inline bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// a float tensor of the call: present, aligned to its elements, rows that do not overlap
+inline bool floats_ok(const void *p, lp_dtype t, size_t cols, size_t ld) { return p && aligned_to(p, dtype_size(t)) && ld >= cols; }
+
+// f(type tag) for the element type of t
+template <typename F>
+void with_type(lp_dtype t, F f)
+{
+    if (t == LP_F32) f((float *)nullptr);
+    else if (t == LP_BF16) f((__bf16 *)nullptr);
+    else f((_Float16 *)nullptr);
+}
 
 // x / d and x % d for 0 <= x < 2^31 with m = floor(2^32 / d) (d = 1: 2^32 - 1) from the host
 __device__ __forceinline__ void piece_place(unsigned x, unsigned d, unsigned m, unsigned &q, unsigned &r)

@@ -203,14 +203,6 @@ __global__ __launch_bounds__(kThreads) void ckpt8_act_bwd_kernel(const v2u *__re
 
 // ---------------------------------------------------------------------------------- launches
 
-// f(type tag) for the element type of t
-template <typename F>
-static void with_type(lp_dtype t, F f)
-{
-    if (t == LP_F32) f((float *)nullptr);
-    else if (t == LP_BF16) f((__bf16 *)nullptr);
-    else f((_Float16 *)nullptr);
-}
 template <typename F>
 static void with_mode(lp_round r, F f)
 {
@@ -258,12 +250,6 @@ extern "C" lp_status lp_ckpt8_bytes(size_t rows, size_t cols, size_t *codes_byte
     *scales_bytes_host = rows * ckpt8_blocks(cols);
     *codes_bytes_host = *scales_bytes_host * 32;
     return LP_OK;
-}
-
-// a float tensor of the call: present, aligned to its elements, rows that do not overlap
-static bool floats_ok(const void *p, lp_dtype t, size_t cols, size_t ld)
-{
-    return p && aligned_to(p, dtype_size(t)) && ld >= cols;
 }
 
 extern "C" lp_status lp_mx4_quantize(const void *x_dev, lp_dtype xt, size_t rows, size_t cols, size_t ldx, void *codes_dev,

@@ -803,7 +803,6 @@ static bool sizes_taken(int M, int K, int Nout)
 }
 
 static bool mx4_ok(const void *codes, const void *scales) { return codes && aligned16(codes) && scales && aligned_to(scales, 8); }
-static bool floats_ok(const void *p, lp_dtype t, size_t cols, size_t ld) { return p && aligned_to(p, dtype_size(t)) && ld >= cols; }
 
 static size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -878,15 +877,6 @@ static Cut cut_product(int I, int J, int stages, int step, int least, const Tile
 }
 
 static unsigned workgroups(const Grid &g) { return (unsigned)g.whole + (unsigned)g.per_xcd * kXCDs; }
-
-// f(type tag) for the element type of t
-template <typename F>
-static void with_type(lp_dtype t, F f)
-{
-    if (t == LP_F32) f((float *)nullptr);
-    else if (t == LP_BF16) f((__bf16 *)nullptr);
-    else f((_Float16 *)nullptr);
-}
 
 // out = act(sum of the parts + bias)
 static void join_parts(const Cut &c, const Grid &g, lp_dtype t, const Sink &out, int I, int J, hipStream_t st)
